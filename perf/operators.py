@@ -1,0 +1,559 @@
+"""Timed cases of two operators next to the KDN mixer: the gated delta rule (the fixed-gain sibling
+of the KDN recurrences: chunked forward, backward and single-token decode) and a step of beam search
+over a pool of recurrent states (selection over beams and vocabulary, reordering of the states).
+
+``listed()`` names the cases, ``draw(rng)`` gives further ones of the same ranges,
+``prepare(case, seed)`` makes a case's inputs on the GPU, ``run(state)`` is one pass (the plain form
+in torch operations where ``own`` is false, the calls of ``paper_2609_07816_amd.kdn`` where it is
+true) and ``exact(case, seed)`` the same outputs in float64.
+
+The sizes follow the mixer layers that the library is built for (16 heads of width 128, training
+context 4096, packed sequences, 256 decode rows), with smaller heads, key heads shared by several
+value heads, ragged lengths and float32 among them.
+
+The gated delta rule, per token of a (sequence, head) with key head h_k = h H_k / H:
+  S_t = alpha_t S_{t-1} + k_t u_t^T,  u_t = beta_t (v_t - alpha_t S_{t-1}^T k_t),
+  o_t = scale S_t^T q_t,  scale = d_k^-1/2.
+
+A step of beam search, per batch element of W beams over V tokens: the candidates (beam w, token y)
+have the score scores[w] + log_softmax(logits[w])[y]; a finished beam has one candidate, its end
+token at its own score. The W best survive: by score, equal ones by beam and, within a beam, by
+logit and then by token, lowest index first. Each beam's recurrent state lives in a slot of a pool:
+a parent's first child keeps its slot, every other child gets the slot of a beam without children
+(in order of the beams) and a copy of its parent's state.
+"""
+
+from __future__ import annotations
+
+import random
+
+import torch
+
+own = False
+DEVICE = "cuda"
+
+# kind: forward, backward, decode (gated delta rule) or beam.
+# n_seq > 0: a packed batch of n_seq sequences with lengths uniform on [lo, hi] (len_seed); then
+# B = 1 and T is unused. state: S0 (and dS_T) are given. decode: B rows in a pool of `slots` states.
+# beam: B batch elements of W beams over V tokens, the states of a Diagonal KDN layer (S and P) in a
+# pool of `slots`; done: some beams are finished; first: the first step, where only beam 0 counts.
+_BASE = dict(kind="forward", dtype="bf16", B=1, T=1, H=16, Hk=16, dk=128, dv=128, state=False,
+             n_seq=0, lo=0, hi=0, len_seed=0, slots=0, W=0, V=0, done=False, first=False)
+
+
+def _case(**kw):
+    c = dict(_BASE)
+    c.update(kw)
+    return c
+
+
+def listed():
+    return [
+        # one layer's forward in training or large prefill
+        _case(name="gdr_fwd_b4_t4096", B=4, T=4096),
+        # a packed batch of prompts or documents of very different lengths, continued from states
+        _case(name="gdr_fwd_packed16", n_seq=16, lo=64, hi=4096, len_seed=3, state=True),
+        # one long prompt alone, ragged length: few chains, each of them long
+        _case(name="gdr_fwd_b1_t8191", T=8191),
+        # one short prompt alone: a call that is all latency
+        _case(name="gdr_fwd_b1_t100", T=100),
+        # float32, smaller heads, two value heads to a key head
+        _case(name="gdr_fwd_f32_b2_t1000_d64", dtype="f32", B=2, T=1000, H=8, Hk=4, dk=64, dv=64,
+              state=True),
+        # one layer's backward in training
+        _case(name="gdr_bwd_b4_t4096", kind="backward", B=4, T=4096),
+        # backward of a packed batch with smaller heads, shared key heads and final-state gradients
+        _case(name="gdr_bwd_packed12_d64", kind="backward", H=8, Hk=4, dk=64, dv=64, n_seq=12,
+              lo=64, hi=2048, len_seed=5, state=True),
+        # one generation step of a full serving batch, rows spread over a state pool
+        _case(name="gdr_dec_r256", kind="decode", B=256, slots=512),
+        # one generation step of a few rows, key heads shared by four value heads
+        _case(name="gdr_dec_r4", kind="decode", B=4, Hk=4, slots=16),
+        # beam search of one request: all latency
+        _case(name="beam_n1_w4", kind="beam", B=1, W=4, V=32000, slots=8),
+        # beam search of a serving batch, some beams finished, odd vocabulary
+        _case(name="beam_n48_w8", kind="beam", B=48, W=8, V=50021, slots=400, done=True),
+        # float32 logits over a large vocabulary
+        _case(name="beam_f32_n16_w5", kind="beam", dtype="f32", B=16, W=5, V=131072, slots=100),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(lo * (hi / lo) ** rng.random()))
+
+
+def draw(rng: random.Random):
+    kind = rng.choice(["forward", "forward", "backward", "decode", "beam", "beam"])
+    c = _case(kind=kind, dtype=rng.choice(["bf16", "bf16", "bf16", "f32"]))
+    if kind == "beam":
+        c.update(B=_log_int(rng, 1, 48), W=rng.randint(2, 8), V=_log_int(rng, 1000, 131072),
+                 done=rng.random() < 0.5, first=rng.random() < 0.2)
+        c["B"] = max(1, min(c["B"], 24000000 // (c["W"] * c["V"])))
+        c["H"] = rng.choice([4, 16])
+        c["Hk"] = c["H"]
+        c["slots"] = c["B"] * c["W"] + rng.randint(0, 16)
+        return c
+    if rng.random() < 0.5:
+        c["Hk"] = rng.choice([16, 16, 8, 4])
+    else:
+        c["H"] = rng.choice([1, 2, 3, 6, 8, 12, 16])
+        c["Hk"] = c["H"] // rng.choice([d for d in (1, 1, 2, 3, 4) if c["H"] % d == 0])
+        c.update(dk=rng.choice([32, 64, 128]), dv=rng.choice([32, 64, 128]))
+    if kind == "decode":
+        c["B"] = _log_int(rng, 1, 256)
+        c["slots"] = c["B"] + rng.randint(0, c["B"])
+        return c
+    c["state"] = rng.random() < 0.5
+    most = 16000 if kind == "forward" else 8000  # tokens in all
+    if c["dtype"] == "f32":
+        most //= 4
+    if rng.random() < 0.4:
+        c["n_seq"] = rng.randint(2, 16)
+        mean = _log_int(rng, 20, max(21, most // c["n_seq"]))
+        c.update(lo=max(1, mean // 4), hi=mean, len_seed=rng.randrange(1 << 20))
+    else:
+        total = _log_int(rng, 33, most)
+        c["B"] = min(rng.choice([1, 1, 2, 4, 8]), total)
+        c["T"] = max(1, min(total // c["B"], 8192))
+    return c
+
+
+# ---------------------------------------------------------------------------------------------
+# inputs
+# ---------------------------------------------------------------------------------------------
+def _lengths(c):
+    g = random.Random(c["len_seed"])
+    return [g.randint(c["lo"], c["hi"]) for _ in range(c["n_seq"])]
+
+
+def _sizes(c):
+    """(B, T, N) of the tensors: one packed row, or B rows of T tokens."""
+    if c["kind"] == "decode":
+        return c["B"], 1, c["B"]
+    if c["n_seq"]:
+        return 1, sum(_lengths(c)), c["n_seq"]
+    return c["B"], c["T"], c["B"]
+
+
+def _dtype(c):
+    return torch.bfloat16 if c["dtype"] == "bf16" else torch.float32
+
+
+def _end_token(c):
+    return min(2, c["V"] - 1)
+
+
+def _inputs(c, seed):
+    g = torch.Generator(device=DEVICE).manual_seed(seed)
+    dt = _dtype(c)
+    H, Hk, dk, dv = c["H"], c["Hk"], c["dk"], c["dv"]
+
+    def normal(*shape):
+        return torch.randn(shape, generator=g, device=DEVICE)
+
+    def uniform(lo, hi, *shape):
+        return lo + (hi - lo) * torch.rand(shape, generator=g, device=DEVICE)
+
+    if c["kind"] == "beam":
+        B, W, V, n = c["B"], c["W"], c["V"], c["slots"]
+        x = {}
+        # logits of a peaked distribution: a few likely tokens, the same ones for most beams
+        peak = 12.0 * uniform(0, 1, B, 1, V) ** 20
+        x["logits"] = (normal(B, W, V) + peak).to(dt)
+        x["scores"] = -uniform(5.0, 12.0, B, W)
+        x["done"] = None
+        if c["done"]:
+            x["done"] = uniform(0, 1, B, W) < 0.2
+        if c["first"]:
+            x["scores"][:, 1:] = float("-inf")
+        x["slot_idx"] = torch.randperm(n, generator=g, device=DEVICE)[:B * W].view(B, W).int()
+        x["S"] = 0.1 * normal(n, H, dk, dv)
+        x["P"] = uniform(0.1, 1.0, n, H, dk)
+        return x
+
+    B, T, N = _sizes(c)
+    x = {}
+    for name in ("q", "k"):
+        t = normal(B, T, Hk, dk)
+        x[name] = (t / t.norm(dim=-1, keepdim=True)).to(dt)
+    x["v"] = normal(B, T, H, dv).to(dt)
+    # gates: per-head rates of 0.01 to 1 per token (log-uniform), modulated by the token
+    rate = torch.exp(uniform(-4.6, 0.0, H))
+    x["alpha"] = torch.exp(-rate * torch.nn.functional.softplus(normal(B, T, H))).to(dt)
+    x["beta"] = torch.sigmoid(normal(B, T, H)).to(dt)
+    x["S0"] = x["cu"] = None
+    if c["kind"] == "decode":
+        n = c["slots"]
+        x["S"] = 0.1 * normal(n, H, dk, dv)
+        x["slot_idx"] = torch.randperm(n, generator=g, device=DEVICE)[:B].int()
+        for name in ("q", "k", "v", "alpha", "beta"):
+            x[name] = x[name].squeeze(1)  # [rows, 1, H, ..] -> [rows, H, ..]
+        x["o"] = torch.empty_like(x["v"])
+        return x
+    if c["state"]:
+        x["S0"] = 0.1 * normal(N, H, dk, dv)
+    if c["n_seq"]:
+        x["cu"] = torch.tensor([0] + _lengths(c)).cumsum(0).int().to(DEVICE)
+    if c["kind"] == "backward":
+        x["dO"] = normal(B, T, H, dv).to(dt)
+        x["dS_T"] = normal(N, H, dk, dv) if c["state"] else None
+    return x
+
+
+def prepare(case, seed):
+    return dict(case=case, x=_inputs(case, seed))
+
+
+# ---------------------------------------------------------------------------------------------
+# the calls of the library
+# ---------------------------------------------------------------------------------------------
+def _run_own(c, x):
+    from paper_2609_07816_amd import kdn
+    if c["kind"] == "beam":
+        scores, token, parent, done = kdn.beam_select(x["logits"], x["scores"], done=x["done"],
+                                                      end_token=_end_token(c))
+        slots = kdn.beam_reorder(parent, x["slot_idx"], x["S"], x["P"])
+        return dict(scores=scores, token=token, parent=parent, done=done, slots=slots, S=x["S"],
+                    P=x["P"])
+    args = [x[n] for n in ("q", "k", "v", "alpha", "beta")]
+    if c["kind"] == "decode":
+        o = kdn.decode_step_gdr(*args, x["S"], slot_idx=x["slot_idx"], o=x["o"])
+        return dict(o=o, S=x["S"])
+    if c["kind"] == "forward":
+        o, S = kdn.forward_gdr(*args, S0=x["S0"], cu_seqlens=x["cu"])
+        return dict(o=o, S=S)
+    return kdn.backward_gdr(*args, S0=x["S0"], cu_seqlens=x["cu"], dO=x["dO"], dS_T=x["dS_T"])
+
+
+# ---------------------------------------------------------------------------------------------
+# the plain forms: float32 torch operations
+# ---------------------------------------------------------------------------------------------
+_CHUNK = 64
+
+
+def _rows(c):
+    """(rows, tokens of a row padded to whole chunks, index of every padded position in the flat
+    tokens, whether it is a token)."""
+    B, T, N = _sizes(c)
+    lens = torch.tensor(_lengths(c) if c["n_seq"] else [T] * N)
+    L = -(-int(lens.max()) // _CHUNK) * _CHUNK
+    start = lens.cumsum(0) - lens
+    pos = torch.arange(L)
+    at = (start[:, None] + pos).clamp(max=B * T - 1)
+    return N, L, at.to(DEVICE), (pos < lens[:, None]).to(DEVICE)
+
+
+def _chains(c, y, heads, rows, fill=0.0):
+    """[B, T, h, ..] -> float32 [N * H, chunks, 64, ..], padded with `fill`, with a key head's rows
+    given to each of its value heads."""
+    N, L, at, live = rows
+    y = y.reshape(-1, *y.shape[2:])[at].float()
+    y = torch.where(live.view(N, L, *[1] * (y.dim() - 2)), y, torch.full_like(y[:1, :1], fill))
+    y = y.repeat_interleave(heads // y.shape[2], dim=2).movedim(2, 1)
+    return y.reshape(N * heads, L // _CHUNK, _CHUNK, *y.shape[3:]).contiguous()
+
+
+def _unchain(c, y, heads, rows, key=False):
+    """The reverse of _chains, rounded to the call's type; key: summed over the value heads that
+    share a key head."""
+    B, T, _ = _sizes(c)
+    N, L, at, live = rows
+    y = y.reshape(N, heads, L, *y.shape[3:]).movedim(1, 2)
+    if key:
+        y = y.reshape(N, L, c["Hk"], heads // c["Hk"], *y.shape[3:]).sum(3)
+    out = torch.zeros((B * T,) + tuple(y.shape[2:]), device=y.device)
+    out[at[live]] = y[live]
+    return out.view(B, T, *out.shape[1:]).to(_dtype(c))
+
+
+def _chunk_matrices(c, x, rows):
+    """Every chunk's operands: with l the cumulative log2 decay, R_ts = 2^(l_t - l_s),
+    L = tril(beta R (K K^T), -1) and its inverse factor Ti = (I + L)^-1, A = tril(R (Q K^T))."""
+    H = c["H"]
+    q, k, v = (_chains(c, x[n], H, rows) for n in ("q", "k", "v"))
+    al, be = _chains(c, x["alpha"], H, rows, 1.0), _chains(c, x["beta"], H, rows)
+    l = torch.log2(al).cumsum(-1)
+    tri = torch.ones(_CHUNK, _CHUNK, device=q.device).tril()
+    R = torch.exp2((l.unsqueeze(-1) - l.unsqueeze(-2)) * tri) * tri
+    kT = k.transpose(-1, -2).contiguous()
+    M = (R * (k @ kT)).tril(-1)
+    L = be.unsqueeze(-1) * M
+    A = R * (q @ kT)
+    Ti = torch.eye(_CHUNK, device=q.device).expand_as(L).clone()
+    for i in range(1, _CHUNK):  # forward substitution, row by row
+        Ti[..., i, :i] = -(L[..., i:i + 1, :i] @ Ti[..., :i, :i]).squeeze(-2)
+    g = torch.exp2(l).unsqueeze(-1)                    # decay since the chunk's start
+    w = torch.exp2(l[..., -1:] - l).unsqueeze(-1)      # decay to its end
+    return dict(q=q, k=k, v=v, al=al, be=be.unsqueeze(-1), R=R, M=M, L=L, A=A, Ti=Ti, g=g, w=w,
+                wkT=(w * k).transpose(-1, -2).contiguous())
+
+
+def _memory_scan(c, x, m, keep):
+    """The forward over the chunks: outputs, final state, and with `keep` each chunk's entering
+    state, innovations' inputs X and writes U."""
+    n, dk, dv = m["k"].shape[0], c["dk"], c["dv"]
+    S = torch.zeros(n, dk, dv, device=m["k"].device)
+    if x["S0"] is not None:
+        S = x["S0"].reshape(n, dk, dv).clone()
+    o, kept = [], []
+    for i in range(m["k"].shape[1]):
+        X = m["v"][:, i] - m["g"][:, i] * (m["k"][:, i] @ S)
+        U = m["Ti"][:, i] @ (m["be"][:, i] * X)
+        if keep:
+            kept.append((S, X, U))
+        else:
+            o.append(m["g"][:, i] * (m["q"][:, i] @ S) + m["A"][:, i] @ U)
+        S = m["g"][:, i, -1:] * S + m["wkT"][:, i] @ U
+    if keep:
+        return [torch.stack(t, 1) for t in zip(*kept)]
+    return torch.stack(o, 1) * dk ** -0.5, S
+
+
+def _forward(c, x):
+    rows = _rows(c)
+    o, S = _memory_scan(c, x, _chunk_matrices(c, x, rows), False)
+    return dict(o=_unchain(c, o, c["H"], rows),
+                S=S.view(-1, c["H"], c["dk"], c["dv"]))
+
+
+def _backward(c, x):
+    rows, H, dk, dv = _rows(c), c["H"], c["dk"], c["dv"]
+    m = _chunk_matrices(c, x, rows)
+    S, X, U = _memory_scan(c, x, m, True)
+    dO = _chains(c, x["dO"], H, rows) * dk ** -0.5
+    n, nc = S.shape[:2]
+    q, k, g, w, be = (m[y] for y in ("q", "k", "g", "w", "be"))
+    AT, TiT = (m[y].transpose(-1, -2).contiguous() for y in ("A", "Ti"))
+    gqT = (g * q).transpose(-1, -2).contiguous()
+    gkT = (g * k).transpose(-1, -2).contiguous()
+    dS = torch.zeros(n, dk, dv, device=S.device)
+    if x["dS_T"] is not None:
+        dS = x["dS_T"].reshape(n, dk, dv).clone()
+    dSs, Ys = [None] * nc, [None] * nc
+    for i in reversed(range(nc)):
+        dU = AT[:, i] @ dO[:, i] + w[:, i] * (k[:, i] @ dS)
+        Y = TiT[:, i] @ dU
+        dSs[i], Ys[i] = dS, Y
+        dS = g[:, i, -1:] * dS + gqT[:, i] @ dO[:, i] - gkT[:, i] @ (be[:, i] * Y)
+    dSo, Y = torch.stack(dSs, 1), torch.stack(Ys, 1)
+    dX = be * Y
+    UT = U.transpose(-1, -2).contiguous()
+    ST, dST = S.transpose(-1, -2).contiguous(), dSo.transpose(-1, -2).contiguous()
+    dA = (dO @ UT).tril()
+    dL = -(Y @ UT).tril(-1)
+    RdA, RdM = m["R"] * dA, m["R"] * be * dL
+    dq_S, dk_S, dk_T = g * (dO @ ST), -g * (dX @ ST), w * (U @ dST)
+    dq = dq_S + RdA @ k
+    dk_ = dk_S + dk_T + RdA.transpose(-1, -2).contiguous() @ q + RdM @ k + \
+        RdM.transpose(-1, -2).contiguous() @ k
+    dbe = (Y * X).sum(-1) + (dL * m["M"]).sum(-1)
+    # the log-decay's gradient: everything that crosses the token, from the state before it to a
+    # read or write at or after it
+    Pm = dA * m["A"] + dL * m["L"]
+    cross = torch.cat([torch.zeros_like(Pm[..., :1]), Pm.cumsum(-1)[..., :-1]], -1)
+    tri = torch.ones(_CHUNK, _CHUNK, device=S.device).tril()
+    dlog = (cross * tri).sum(-2)
+    reads = (q * dq_S + k * dk_S).sum(-1)
+    dlog = dlog + reads.flip(-1).cumsum(-1).flip(-1)
+    writes = (k * dk_T).sum(-1)
+    dlog = dlog + writes.cumsum(-1) - writes
+    dlog = dlog + g[..., -1, :] * (S * dSo).sum((-1, -2)).unsqueeze(-1)
+    return dict(dq=_unchain(c, dq, H, rows, key=True), dk=_unchain(c, dk_, H, rows, key=True),
+                dv=_unchain(c, dX, H, rows), dalpha=_unchain(c, dlog / m["al"], H, rows),
+                dbeta=_unchain(c, dbe, H, rows), dS0=dS.view(-1, H, dk, dv))
+
+
+def _decode(c, x):
+    rep = c["H"] // c["Hk"]
+    q, k = (x[n].float().repeat_interleave(rep, dim=1).unsqueeze(-1) for n in ("q", "k"))
+    at = x["slot_idx"].long()
+    S = x["S"][at] * x["alpha"].float()[..., None, None]
+    u = x["beta"].float().unsqueeze(-1) * (x["v"].float() - (S * k).sum(-2))
+    S = S + k * u.unsqueeze(-2)
+    x["S"][at] = S
+    return dict(o=((S * q).sum(-2) * c["dk"] ** -0.5).to(_dtype(c)), S=x["S"])
+
+
+def _best(x, ids, W):
+    """The W largest of each row of x, in order, ties by the lowest place: (values, ids there)."""
+    x, values, found = x.clone(), [], []
+    place = torch.arange(x.shape[-1], device=x.device)
+    alive = torch.ones_like(x, dtype=torch.bool)
+    for _ in range(W):
+        top = torch.where(alive, x, float("-inf")).amax(-1, keepdim=True)
+        first = torch.where(alive & (x == top), place, x.shape[-1]).amin(-1, keepdim=True)
+        values.append(top)
+        found.append(ids.gather(-1, first))
+        alive &= place != first
+    return torch.cat(values, -1), torch.cat(found, -1)
+
+
+def _beam(c, x):
+    B, W, V = c["B"], c["W"], c["V"]
+    y = x["logits"].float()
+    token = torch.arange(V, device=y.device).expand(B, W, V)
+    top = y.amax(-1, keepdim=True)
+    lse = top + torch.log(torch.exp(y - top).sum(-1, keepdim=True))
+    if x["done"] is not None:  # a finished beam goes on with its end token only, at its own score
+        end = torch.where(token == _end_token(c), 0.0, float("-inf"))
+        y = torch.where(x["done"].unsqueeze(-1), end, y)
+        lse = torch.where(x["done"].unsqueeze(-1), torch.zeros_like(lse), lse)
+    y, token = _best(y, token, min(W, V))
+    score = (x["scores"].unsqueeze(-1) + (y - lse)).flatten(1)
+    scores, at = _best(score, torch.arange(score.shape[-1], device=y.device).expand_as(score), W)
+    parent = at // y.shape[-1]
+    token = token.flatten(1).gather(-1, at)
+    done = token == _end_token(c)
+    if x["done"] is not None:
+        done |= x["done"].gather(-1, parent)
+    # slots: a parent's first child keeps its slot, the others get those of childless beams
+    beam = torch.arange(W, device=y.device)
+    same = parent.unsqueeze(-1) == parent.unsqueeze(-2)
+    later = (same & (beam < beam.unsqueeze(-1))).any(-1)
+    free = ~(parent.unsqueeze(-1) == beam).any(-2)
+    match = later.unsqueeze(-1) & free.unsqueeze(-2) & (
+        later.cumsum(-1).unsqueeze(-1) == free.cumsum(-1).unsqueeze(-2))
+    slot = x["slot_idx"].long()
+    src = slot.gather(-1, parent)
+    to = torch.where(later, (match * slot.unsqueeze(-2)).sum(-1), src)
+    for pool in (x["S"], x["P"]):
+        pool[to.flatten()] = pool[src.flatten()]
+    return dict(scores=scores, token=token.int(), parent=parent.int(), done=done, slots=to.int(),
+                S=x["S"], P=x["P"])
+
+
+def run(state):
+    c, x = state["case"], state["x"]
+    if own:
+        return _run_own(c, x)
+    return dict(forward=_forward, backward=_backward, decode=_decode, beam=_beam)[c["kind"]](c, x)
+
+
+# ---------------------------------------------------------------------------------------------
+# what a pass cannot do without
+# ---------------------------------------------------------------------------------------------
+def work(case):
+    c = case
+    H, Hk, dk, dv, es = c["H"], c["Hk"], c["dk"], c["dv"], 2 if c["dtype"] == "bf16" else 4
+    if c["kind"] == "beam":
+        B, W, V = c["B"], c["W"], c["V"]
+        slot = H * dk * (dv + 1) * 4
+        # copies: beams whose parent has an earlier child; for parents drawn evenly
+        # W (1 - 1/W)^W of W, a third of them
+        copies = B * W * (1 - 1 / W) ** W
+        return dict(bytes=B * W * V * es + B * W * 22 + 2 * copies * slot, flops=B * W * V * 3)
+    B, T, N = _sizes(c)
+    n, S = B * T, N * H * dk * dv * 4
+    ins = n * es * (2 * Hk * dk + H * dv + 2 * H)
+    if c["kind"] == "decode":
+        return dict(bytes=ins + n * H * dv * es + 2 * S, flops=n * H * 6 * dk * dv)
+    if c["kind"] == "forward":
+        return dict(bytes=ins + n * H * dv * es + S * (2 if c["state"] else 1),
+                    flops=n * H * 6 * dk * dv)
+    return dict(bytes=2 * ins + n * H * dv * es + S * (3 if c["state"] else 1),
+                flops=n * H * 16 * dk * dv)
+
+
+# ---------------------------------------------------------------------------------------------
+# float64: token by token
+# ---------------------------------------------------------------------------------------------
+def _step64(S, q, k, v, al, be):
+    """One token of every chain: S [n, H, dk, dv], the rest [n, H, ..]."""
+    S = al[..., None, None] * S
+    u = be[..., None] * (v - torch.einsum("nhij,nhi->nhj", S, k))
+    S = S + k.unsqueeze(-1) * u.unsqueeze(-2)
+    return S, torch.einsum("nhij,nhi->nhj", S, q) * q.shape[-1] ** -0.5
+
+
+def _padded64(c, x, names):
+    """[n, L, heads, ..] float64 rows of sequences, padded with tokens that change nothing."""
+    lens = _lengths(c) if c["n_seq"] else [c["T"]] * c["B"]
+    out = {}
+    for name in names:
+        y = x[name].double()
+        if c["n_seq"]:
+            pad = torch.full((len(lens), max(lens)) + tuple(y.shape[2:]),
+                             1.0 if name == "alpha" else 0.0, dtype=torch.float64,
+                             device=y.device)
+            at = 0
+            for i, ln in enumerate(lens):
+                pad[i, :ln] = y[0, at:at + ln]
+                at += ln
+            y = pad
+        out[name] = y
+    return out, lens
+
+
+def _flat64(c, y, lens):
+    if not c["n_seq"]:
+        return y
+    return torch.cat([y[i, :ln] for i, ln in enumerate(lens)], 0).unsqueeze(0)
+
+
+def _exact_beam(c, x):
+    """Scores of the selection and the moved pools; the whole numbers come from the plain form's
+    definition, found here by sorting."""
+    B, W, V = c["B"], c["W"], c["V"]
+    logp = x["logits"].double()
+    logp = logp - torch.logsumexp(logp, -1, keepdim=True)
+    if x["done"] is not None:
+        end = torch.full((V,), float("-inf"), dtype=torch.float64, device=logp.device)
+        end[_end_token(c)] = 0.0
+        logp = torch.where(x["done"].unsqueeze(-1), end, logp)
+    total = (x["scores"].double().unsqueeze(-1) + logp).flatten(1)
+    best, at = total.topk(W, dim=-1)
+    return dict(scores=best, token=None, parent=None, done=None, slots=None, S=None, P=None)
+
+
+def exact(case, seed):
+    c, x = case, _inputs(case, seed)
+    if c["kind"] == "beam":
+        return _exact_beam(c, x)
+    H, dk, dv = c["H"], c["dk"], c["dv"]
+    rep = H // c["Hk"]
+    names = ("q", "k", "v", "alpha", "beta")
+    if c["kind"] == "decode":
+        t = [x[n].double() for n in names]
+        t[0], t[1] = (y.repeat_interleave(rep, dim=1) for y in t[:2])
+        at = x["slot_idx"].long()
+        pool = x["S"].double()
+        pool[at], o = _step64(pool[at], *t)
+        return dict(o=o, S=pool)
+    back = c["kind"] == "backward"
+    t, lens = _padded64(c, x, names + (("dO",) if back else ()))
+    n, L = t["v"].shape[:2]
+    S = torch.zeros(n, H, dk, dv, dtype=torch.float64, device=t["v"].device)
+    if x["S0"] is not None:
+        S = x["S0"].double()
+
+    def token(y, i):
+        return y[:, i].repeat_interleave(H // y.shape[2], dim=1)
+
+    if not back:
+        o = torch.zeros(n, L, H, dv, dtype=torch.float64, device=S.device)
+        for i in range(L):
+            S, o[:, i] = _step64(S, *[token(t[m], i) for m in names])
+        return dict(o=_flat64(c, o, lens), S=S)
+    # states at every 32nd token, then each span again under autograd, last one first
+    span, kept = 32, []
+    for i in range(L):
+        if i % span == 0:
+            kept.append(S)
+        S, _ = _step64(S, *[token(t[m], i) for m in names])
+    gS = x["dS_T"].double() if x["dS_T"] is not None else torch.zeros_like(S)
+    grads = {m: torch.zeros_like(t[m]) for m in names}
+    for j in reversed(range(len(kept))):
+        i0, i1 = j * span, min((j + 1) * span, L)
+        leaf = [t[m][:, i0:i1].clone().requires_grad_() for m in names]
+        S0 = kept[j].clone().requires_grad_()
+        S, loss = S0, 0.0
+        for i in range(i1 - i0):
+            S, o = _step64(S, *[token(y, i) for y in leaf])
+            loss = loss + (o * t["dO"][:, i0 + i]).sum()
+        got = torch.autograd.grad(loss + (S * gS).sum(), leaf + [S0])
+        for m, y in zip(names, got):
+            grads[m][:, i0:i1] = y
+        gS, kept[j] = got[-1], None
+    out = {"d" + m: _flat64(c, grads[m], lens) for m in names}
+    out["dS0"] = gS
+    return out
