@@ -393,13 +393,13 @@ def _beam(c, x):
     y = x["logits"].float()
     token = torch.arange(V, device=y.device).expand(B, W, V)
     top = y.amax(-1, keepdim=True)
-    lse = top + torch.log(torch.exp(y - top).sum(-1, keepdim=True))
+    norm = torch.log(torch.exp(y - top).sum(-1, keepdim=True))
     if x["done"] is not None:  # a finished beam goes on with its end token only, at its own score
         end = torch.where(token == _end_token(c), 0.0, float("-inf"))
         y = torch.where(x["done"].unsqueeze(-1), end, y)
-        lse = torch.where(x["done"].unsqueeze(-1), torch.zeros_like(lse), lse)
+        top, norm = (torch.where(x["done"].unsqueeze(-1), 0.0, t) for t in (top, norm))
     y, token = _best(y, token, min(W, V))
-    score = (x["scores"].unsqueeze(-1) + (y - lse)).flatten(1)
+    score = (x["scores"].unsqueeze(-1) + ((y - top) - norm)).flatten(1)
     scores, at = _best(score, torch.arange(score.shape[-1], device=y.device).expand_as(score), W)
     parent = at // y.shape[-1]
     token = token.flatten(1).gather(-1, at)
