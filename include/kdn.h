@@ -316,6 +316,85 @@ kdn_status_t kdn_forward_kam(const void* q, const void* k, const void* v, const 
                              int32_t N, int32_t B, int32_t T, int32_t H, int32_t dk, int32_t dv,
                              kdn_dtype_t dtype, float scale, void* stream);
 
+/*
+ * Gated delta rule: the delta rule with a given gain and one decay per head (the fixed-gain filter
+ * that Sec. "Delta-rule models as fixed-gain Kalman filters" starts from). Per token of a (sequence,
+ * head):
+ *   u = beta (v - alpha S^T k);  S = alpha S + k u^T;  o = scale * S^T q
+ *   q, k: [B,T,Hk,dk], Hk key heads, Hk dividing H: value head h reads key head h / (H / Hk)
+ *   v, o: [B,T,H,dv]; alpha, beta: [B,T,H]   (dtype)
+ *   S0, S_T: [N,H,dk,dv] float32 (S0 NULL = 0; S_T NULL = not written; S_T may alias S0 exactly)
+ *   0 <= alpha <= 1 (a gate of 0 clears the memory); beta is any real number, usually in [0, 1]
+ *   or [0, 2]; scale > 0. q and k are taken as given, not normalised.
+ *   workspace: kdn_forward_gdr_workspace_bytes(...) bytes (may be 0), 16-byte aligned, no
+ *   initialisation needed.
+ * Packing, alignment, asynchrony and errors as for kdn_forward_diag; there is no limit of 2 GiB on
+ * a tensor. o must overlap no input and no state.
+ */
+kdn_status_t kdn_forward_gdr(const void* q, const void* k, const void* v, const void* alpha,
+                             const void* beta, const float* S0, void* o, float* S_T,
+                             const int32_t* cu_seqlens, int32_t N, int32_t B, int32_t T, int32_t H,
+                             int32_t Hk, int32_t dk, int32_t dv, kdn_dtype_t dtype, float scale,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
+/* Device scratch (bytes) kdn_forward_gdr needs (packed != 0 with cu_seqlens); 0 for arguments it
+ * rejects.                                                                                     */
+size_t kdn_forward_gdr_workspace_bytes(int32_t N, int32_t B, int32_t T, int32_t H, int32_t Hk,
+                                       int32_t dk, int32_t dv, kdn_dtype_t dtype, int32_t packed);
+
+/*
+ * One token of the gated delta rule per row, the state resident in a slot pool and updated in
+ * place: q, k [R,Hk,dk]; v, o [R,H,dv]; alpha, beta [R,H] (dtype); S [num_slots,H,dk,dv] float32;
+ * slot_idx as in kdn_decode_step (NULL: row i uses slot i; a row whose slot is negative or
+ * >= num_slots is skipped, its o left as it is; two rows naming the same slot race).
+ */
+kdn_status_t kdn_decode_step_gdr(const void* q, const void* k, const void* v, const void* alpha,
+                                 const void* beta, float* S, const int32_t* slot_idx, void* o,
+                                 int32_t R, int32_t num_slots, int32_t H, int32_t Hk, int32_t dk,
+                                 int32_t dv, kdn_dtype_t dtype, float scale, void* stream);
+
+/*
+ * One selection step of beam search: per batch element, the W best of W x V candidates.
+ *   logits [N,W,V] (dtype, any alignment of its element); scores [N,W] float32, the beams' scores
+ *   so far (-inf: the beam does not count, as all but the first at the first step); done [N,W] bytes
+ *   or NULL: a beam with done != 0 is finished, and its one candidate is `end_token` at its own
+ *   score. Candidate (w, y) of another beam has the score scores[w] + log_softmax(logits[w])[y],
+ *   computed in float32.
+ *   scores_out, token, parent [N,W]: the W best in order, with the beam each continues; done_out
+ *   [N,W] bytes or NULL: the parent is done or the token is end_token. No output may overlap another
+ *   or an input.
+ *   Order: by score, equal scores by beam, and within a beam by logit, then by token, lowest first
+ *   (a finished beam's other tokens follow with -inf in token order). A NaN logit counts as -inf, +inf
+ *   as the largest finite value. All W x V candidates take part, those of score -inf too, so
+ *   there are always W of them.
+ *   W <= 64, N W <= 65535 (KDN_ERR_UNSUPPORTED otherwise).
+ *   workspace: kdn_beam_select_workspace_bytes(...) bytes, 16-byte aligned.
+ */
+kdn_status_t kdn_beam_select(const void* logits, const float* scores, const uint8_t* done, int32_t N,
+                             int32_t W, int32_t V, kdn_dtype_t dtype, int32_t end_token,
+                             float* scores_out, int32_t* token, int32_t* parent, uint8_t* done_out,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
+/* Device scratch (bytes) kdn_beam_select needs; 0 for sizes it rejects.                        */
+size_t kdn_beam_select_workspace_bytes(int32_t N, int32_t W, int32_t V);
+
+/*
+ * Moves the beams' recurrent states after a selection: slot_out [N,W] gets the slot of every new
+ * beam, and the pool S (and P, or NULL) of num_slots states of s_slot_bytes (p_slot_bytes) each is
+ * updated in place. A parent's first child keeps the parent's slot; every other child gets the slot
+ * of a beam without children (the i-th such child the i-th such beam, in order) and a copy of its
+ * parent's state. Only forked states are copied. With several layers, the call is made for each
+ * layer's pools with the same parent and slot_idx (each gives the same slot_out).
+ *   parent, slot_idx, slot_out: int32 [N,W]. A parent outside [0, W) stands for none: the child
+ *   gets a slot and no copy. A slot outside [0, num_slots) is handed on like another and nothing is
+ *   copied from or to it. slot_out must not overlap slot_idx. The slots of slot_idx must differ.
+ *   Pools and slot sizes are multiples of 4 bytes (16 for copies in 16-byte pieces). W <= 64, N W <=
+ *   65535.
+ */
+kdn_status_t kdn_beam_reorder(const int32_t* parent, const int32_t* slot_idx, int32_t* slot_out,
+                              int32_t N, int32_t W, int32_t num_slots, void* S,
+                              size_t s_slot_bytes, void* P, size_t p_slot_bytes, void* stream);
+
 /* Static text for a status code.                                                             */
 const char* kdn_status_string(kdn_status_t status);
 

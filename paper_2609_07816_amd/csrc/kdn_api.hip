@@ -6,11 +6,7 @@
 
 #include <mutex>
 
-#include "kdn_internal.h"
-
-#include <cstdint>
-#include <initializer_list>
-#include <utility>
+#include "kdn_check.h"
 
 namespace {
 
@@ -25,7 +21,10 @@ void* g_scratch_ptr[MAX_DEVICES] = {};
 
 thread_local char g_err[512] = "";
 
-kdn_status_t fail(kdn_status_t st, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+}  // namespace
+
+// Checks shared with the other entry points (kdn_check.h).
+namespace kdn {
 
 kdn_status_t fail(kdn_status_t st, const char* fmt, ...)
 {
@@ -42,11 +41,6 @@ kdn_status_t ok()
     return KDN_OK;
 }
 
-bool head_ok(int d) { return d == 16 || d == 32 || d == 64 || d == 128; }
-
-size_t esize(kdn_dtype_t dt) { return dt == KDN_F32 ? 4 : 2; }
-
-// Byte ranges [p, p + n) and [q, q + m) overlap.
 bool overlaps(const void* p, size_t n, const void* q, size_t m)
 {
     if (!p || !q || n == 0 || m == 0) return false;
@@ -59,6 +53,34 @@ kdn_status_t hip_status(hipError_t e, const char* what)
     if (e == hipSuccess) return ok();
     return fail(KDN_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
+
+kdn_status_t check_aligned(std::initializer_list<std::pair<const void*, const char*>> ptrs)
+{
+    for (const auto& p : ptrs)
+        if (p.first && ((uintptr_t)p.first & 15))
+            return fail(KDN_ERR_INVALID_ARG, "%s must be 16-byte aligned", p.second);
+    return KDN_OK;
+}
+
+kdn_status_t check_seq(const int32_t* cu, int32_t N, int32_t B, int32_t T, int32_t H)
+{
+    if (B <= 0 || T <= 0 || H <= 0 || N <= 0)
+        return fail(KDN_ERR_INVALID_ARG, "sizes must be positive (N=%d B=%d T=%d H=%d)", N, B,
+                    T, H);
+    if (cu && B != 1)
+        return fail(KDN_ERR_INVALID_ARG, "packed batches (cu_seqlens) need B == 1, got %d", B);
+    if (!cu && N != B)
+        return fail(KDN_ERR_INVALID_ARG, "without cu_seqlens N must equal B (N=%d B=%d)", N, B);
+    if ((int64_t)B * T * H > ((int64_t)1 << 31) / 128)
+        return fail(KDN_ERR_INVALID_ARG, "B*T*H too large for 32-bit token indexing");
+    return KDN_OK;
+}
+
+}  // namespace kdn
+
+namespace {
+
+using namespace kdn;
 
 // Device address of the current device's copy of `scratch`, looked up once per device.
 kdn_status_t scratch_on_current_device(void** out)
@@ -78,31 +100,6 @@ kdn_status_t scratch_on_current_device(void** out)
         g_scratch_ptr[dev] = p;
     }
     *out = g_scratch_ptr[dev];
-    return KDN_OK;
-}
-
-// Tensors whose innermost dimension is d_k or d_v are read and written in 16-byte pieces: each
-// must start at a 16-byte boundary (null pointers are skipped).
-kdn_status_t check_aligned(std::initializer_list<std::pair<const void*, const char*>> ptrs)
-{
-    for (const auto& p : ptrs)
-        if (p.first && ((uintptr_t)p.first & 15))
-            return fail(KDN_ERR_INVALID_ARG, "%s must be 16-byte aligned", p.second);
-    return KDN_OK;
-}
-
-// Shared validation of the forward / gain argument sets.
-kdn_status_t check_seq(const int32_t* cu, int32_t N, int32_t B, int32_t T, int32_t H)
-{
-    if (B <= 0 || T <= 0 || H <= 0 || N <= 0)
-        return fail(KDN_ERR_INVALID_ARG, "sizes must be positive (N=%d B=%d T=%d H=%d)", N, B,
-                    T, H);
-    if (cu && B != 1)
-        return fail(KDN_ERR_INVALID_ARG, "packed batches (cu_seqlens) need B == 1, got %d", B);
-    if (!cu && N != B)
-        return fail(KDN_ERR_INVALID_ARG, "without cu_seqlens N must equal B (N=%d B=%d)", N, B);
-    if ((int64_t)B * T * H > ((int64_t)1 << 31) / 128)
-        return fail(KDN_ERR_INVALID_ARG, "B*T*H too large for 32-bit token indexing");
     return KDN_OK;
 }
 

@@ -1,0 +1,102 @@
+// C ABI of beam search: host-side argument checks and dispatch.
+#include "kdn_beam.h"
+#include "kdn_check.h"
+
+namespace {
+
+using namespace kdn;
+
+// Grid sizes and 32-bit token indexes bound the rows and the vocabulary.
+bool beam_sizes(int32_t N, int32_t W, int32_t V)
+{
+    return N > 0 && W > 0 && W <= BEAM_MAX && (int64_t)N * W <= 65535 && V > 0 &&
+           V <= ((int32_t)1 << 30);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t kdn_beam_select_workspace_bytes(int32_t N, int32_t W, int32_t V)
+{
+    return beam_sizes(N, W, V) ? beam_workspace_bytes(N, W, V) : 0;
+}
+
+kdn_status_t kdn_beam_select(const void* logits, const float* scores, const uint8_t* done, int32_t N,
+                             int32_t W, int32_t V, kdn_dtype_t dtype, int32_t end_token,
+                             float* scores_out, int32_t* token, int32_t* parent, uint8_t* done_out,
+                             void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!logits || !scores || !scores_out || !token || !parent)
+        return fail(KDN_ERR_INVALID_ARG,
+                    "null required pointer (logits, scores, scores_out, token, parent)");
+    if (dtype != KDN_F32 && dtype != KDN_BF16)
+        return fail(KDN_ERR_INVALID_ARG, "unknown dtype %d", (int)dtype);
+    if (N <= 0 || W <= 0 || V <= 0)
+        return fail(KDN_ERR_INVALID_ARG, "sizes must be positive (N=%d W=%d V=%d)", N, W, V);
+    if (!beam_sizes(N, W, V))
+        return fail(KDN_ERR_UNSUPPORTED, "N=%d W=%d V=%d: at most %d beams, 65535 rows and 2^30 "
+                    "tokens", N, W, V, BEAM_MAX);
+    if (end_token < 0 || end_token >= V)
+        return fail(KDN_ERR_INVALID_ARG, "end_token %d outside the vocabulary of %d", end_token, V);
+    const size_t es = esize(dtype), rows = (size_t)N * W;
+    if ((uintptr_t)logits % es) return fail(KDN_ERR_INVALID_ARG, "logits are misaligned");
+    const void* ins[4] = {logits, scores, done, workspace};
+    const size_t insz[4] = {rows * V * es, rows * 4, rows, workspace_bytes};
+    const void* outs[4] = {scores_out, token, parent, done_out};
+    const size_t osz[4] = {rows * 4, rows * 4, rows * 4, rows};
+    // the outputs are written while other batch elements are still read
+    for (int o = 0; o < 4; ++o) {
+        for (int i = 0; i < 4; ++i)
+            if (overlaps(outs[o], osz[o], ins[i], insz[i]))
+                return fail(KDN_ERR_INVALID_ARG, "output %d overlaps argument buffer %d", o, i);
+        for (int p = 0; p < o; ++p)
+            if (overlaps(outs[o], osz[o], outs[p], osz[p]))
+                return fail(KDN_ERR_INVALID_ARG, "outputs %d and %d overlap", p, o);
+    }
+    const size_t need = beam_workspace_bytes(N, W, V);
+    if (!workspace || workspace_bytes < need)
+        return fail(KDN_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need,
+                    workspace ? workspace_bytes : (size_t)0);
+    if ((uintptr_t)workspace & 15)
+        return fail(KDN_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+    return hip_status(launch_beam_select(logits, scores, done, N, W, V, dtype, end_token,
+                                         scores_out, token, parent, done_out, workspace,
+                                         (hipStream_t)stream),
+                      "kdn_beam_select launch");
+}
+
+kdn_status_t kdn_beam_reorder(const int32_t* parent, const int32_t* slot_idx, int32_t* slot_out,
+                              int32_t N, int32_t W, int32_t num_slots, void* S,
+                              size_t s_slot_bytes, void* P, size_t p_slot_bytes, void* stream)
+{
+    if (!parent || !slot_idx || !slot_out || !S)
+        return fail(KDN_ERR_INVALID_ARG, "null required pointer (parent, slot_idx, slot_out, S)");
+    if (N <= 0 || W <= 0 || num_slots <= 0 || s_slot_bytes == 0 || (P && p_slot_bytes == 0))
+        return fail(KDN_ERR_INVALID_ARG, "sizes must be positive (N=%d W=%d num_slots=%d)", N, W,
+                    num_slots);
+    if (!beam_sizes(N, W, 1))
+        return fail(KDN_ERR_UNSUPPORTED, "N=%d W=%d: at most %d beams and 65535 rows", N, W,
+                    BEAM_MAX);
+    if (s_slot_bytes > ((size_t)1 << 40) || p_slot_bytes > ((size_t)1 << 40))
+        return fail(KDN_ERR_UNSUPPORTED, "a slot of more than 2^40 bytes");
+    if ((s_slot_bytes | (P ? p_slot_bytes : 0) | (uintptr_t)S | (uintptr_t)P) & 3)
+        return fail(KDN_ERR_INVALID_ARG, "pools and slot sizes must be multiples of 4 bytes");
+    const size_t rows = (size_t)N * W * 4;
+    const size_t ns = (size_t)num_slots * s_slot_bytes, np = (size_t)num_slots * p_slot_bytes;
+    const void* bufs[4] = {parent, slot_idx, S, P};
+    const size_t bsz[4] = {rows, rows, ns, P ? np : 0};
+    for (int i = 0; i < 4; ++i)
+        if (overlaps(slot_out, rows, bufs[i], bsz[i]))
+            return fail(KDN_ERR_INVALID_ARG, "slot_out overlaps argument buffer %d", i);
+    for (int i = 0; i < 2; ++i)
+        if (overlaps(bufs[i], rows, S, ns) || overlaps(bufs[i], rows, P, P ? np : 0))
+            return fail(KDN_ERR_INVALID_ARG, "a pool overlaps input %d", i);
+    if (overlaps(S, ns, P, P ? np : 0))
+        return fail(KDN_ERR_INVALID_ARG, "S and P must not overlap");
+    return hip_status(launch_beam_reorder(parent, slot_idx, slot_out, N, W, num_slots, S,
+                                          s_slot_bytes, P, p_slot_bytes, (hipStream_t)stream),
+                      "kdn_beam_reorder launch");
+}
+
+}  // extern "C"

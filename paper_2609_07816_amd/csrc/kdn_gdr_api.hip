@@ -1,0 +1,101 @@
+// C ABI of the gated delta rule: host-side argument checks and dispatch. Nothing here reads device
+// memory or synchronizes.
+#include "kdn_check.h"
+#include "kdn_gdr.h"
+
+namespace {
+
+using namespace kdn;
+
+kdn_status_t check_heads(int32_t H, int32_t Hk, int32_t dk, int32_t dv, kdn_dtype_t dtype,
+                         float scale)
+{
+    if (dtype != KDN_F32 && dtype != KDN_BF16)
+        return fail(KDN_ERR_INVALID_ARG, "unknown dtype %d", (int)dtype);
+    if (H <= 0 || Hk <= 0 || H % Hk != 0)
+        return fail(KDN_ERR_INVALID_ARG, "Hk=%d key heads must divide H=%d value heads", Hk, H);
+    if (!head_ok(dk) || !head_ok(dv))
+        return fail(KDN_ERR_UNSUPPORTED, "dk=%d dv=%d: head sizes must be 16, 32, 64 or 128", dk,
+                    dv);
+    if (!(scale > 0.f)) return fail(KDN_ERR_INVALID_ARG, "scale must be positive (%g)", scale);
+    return KDN_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+kdn_status_t kdn_decode_step_gdr(const void* q, const void* k, const void* v, const void* alpha,
+                                 const void* beta, float* S, const int32_t* slot_idx, void* o,
+                                 int32_t R, int32_t num_slots, int32_t H, int32_t Hk, int32_t dk,
+                                 int32_t dv, kdn_dtype_t dtype, float scale, void* stream)
+{
+    if (!q || !k || !v || !alpha || !beta || !S || !o)
+        return fail(KDN_ERR_INVALID_ARG, "null required pointer (q, k, v, alpha, beta, S, o)");
+    kdn_status_t st = check_heads(H, Hk, dk, dv, dtype, scale);
+    if (st != KDN_OK) return st;
+    if (R < 0 || num_slots <= 0 || (int64_t)R * H > ((int64_t)1 << 31) / 128)
+        return fail(KDN_ERR_INVALID_ARG, "bad sizes (R=%d num_slots=%d H=%d)", R, num_slots, H);
+    if (!slot_idx && R > num_slots)
+        return fail(KDN_ERR_INVALID_ARG, "without slot_idx R (%d) must not exceed num_slots (%d)",
+                    R, num_slots);
+    st = check_aligned({{q, "q"}, {k, "k"}, {v, "v"}, {o, "o"}, {S, "S"}});
+    if (st != KDN_OK) return st;
+    const size_t es = esize(dtype), nk = (size_t)R * Hk * dk * es, nv = (size_t)R * H * dv * es;
+    const size_t ng = (size_t)R * H * es, ns = (size_t)num_slots * H * dk * dv * 4;
+    const void* ins[6] = {q, k, v, alpha, beta, slot_idx};
+    const size_t insz[6] = {nk, nk, nv, ng, ng, slot_idx ? (size_t)R * 4 : 0};
+    for (int i = 0; i < 6; ++i)
+        if (overlaps(o, nv, ins[i], insz[i]) || overlaps(S, ns, ins[i], insz[i]))
+            return fail(KDN_ERR_INVALID_ARG, "o or S overlaps input %d", i);
+    if (overlaps(o, nv, S, ns)) return fail(KDN_ERR_INVALID_ARG, "o and S must not overlap");
+    return hip_status(launch_gdr_decode(q, k, v, alpha, beta, S, slot_idx, o, R, num_slots, H, Hk,
+                                        dk, dv, dtype, scale, (hipStream_t)stream),
+                      "kdn_decode_step_gdr launch");
+}
+
+size_t kdn_forward_gdr_workspace_bytes(int32_t N, int32_t B, int32_t T, int32_t H, int32_t Hk,
+                                       int32_t dk, int32_t dv, kdn_dtype_t dtype, int32_t packed)
+{
+    (void)N; (void)B; (void)T; (void)H; (void)Hk; (void)dk; (void)dv; (void)dtype; (void)packed;
+    return 0;
+}
+
+kdn_status_t kdn_forward_gdr(const void* q, const void* k, const void* v, const void* alpha,
+                             const void* beta, const float* S0, void* o, float* S_T,
+                             const int32_t* cu_seqlens, int32_t N, int32_t B, int32_t T, int32_t H,
+                             int32_t Hk, int32_t dk, int32_t dv, kdn_dtype_t dtype, float scale,
+                             void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!q || !k || !v || !alpha || !beta || !o)
+        return fail(KDN_ERR_INVALID_ARG, "null required pointer (q, k, v, alpha, beta, o)");
+    kdn_status_t st = check_heads(H, Hk, dk, dv, dtype, scale);
+    if (st == KDN_OK) st = check_seq(cu_seqlens, N, B, T, H);
+    if (st == KDN_OK)
+        st = check_aligned({{q, "q"}, {k, "k"}, {v, "v"}, {o, "o"}, {S0, "S0"}, {S_T, "S_T"}});
+    if (st != KDN_OK) return st;
+    const size_t es = esize(dtype), rows = (size_t)B * T, ns = (size_t)N * H * dk * dv * 4;
+    const size_t nk = rows * Hk * dk * es, nv = rows * H * dv * es, ng = rows * H * es;
+    const void* ins[6] = {q, k, v, alpha, beta, cu_seqlens};
+    const size_t insz[6] = {nk, nk, nv, ng, ng, cu_seqlens ? (size_t)(N + 1) * 4 : 0};
+    for (int i = 0; i < 6; ++i)
+        if (overlaps(o, nv, ins[i], insz[i]) || overlaps(S_T, ns, ins[i], insz[i]))
+            return fail(KDN_ERR_INVALID_ARG, "o or S_T overlaps input %d", i);
+    if (S_T && S_T != S0 && overlaps(S_T, ns, S0, ns))
+        return fail(KDN_ERR_INVALID_ARG, "S_T partially overlaps S0 (only exact aliasing is "
+                                         "allowed)");
+    if (overlaps(o, nv, S_T, ns) || overlaps(o, nv, S0, ns))
+        return fail(KDN_ERR_INVALID_ARG, "o overlaps a state");
+    const size_t need =
+        kdn_forward_gdr_workspace_bytes(N, B, T, H, Hk, dk, dv, dtype, cu_seqlens != nullptr);
+    if (need > 0 && (!workspace || workspace_bytes < need))
+        return fail(KDN_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need,
+                    workspace ? workspace_bytes : (size_t)0);
+    if (overlaps(workspace, workspace_bytes, o, nv) || overlaps(workspace, workspace_bytes, S_T, ns))
+        return fail(KDN_ERR_INVALID_ARG, "the workspace overlaps an output");
+    const GdrCall c = {q, k, v, alpha, beta, S0, o, S_T, {cu_seqlens, N, B, T, H}, Hk, dk, dv,
+                       dtype, scale, workspace};
+    return hip_status(launch_gdr_recurrent(c, (hipStream_t)stream), "kdn_forward_gdr launch");
+}
+
+}  // extern "C"

@@ -22,6 +22,14 @@ Functions mirror the C entry points:
   scale=None, dO=None, dS_T=None, dP_T=None) -> dict`` of float32 gradients
 * ``forward_kam(q, k, v, alpha, omega, r, S0=None, P0=None, cu_seqlens=None, scale=None)
   -> (o, S_T, P_T)`` -- the dense-covariance Kalman Associative Memory
+* ``forward_gdr(q, k, v, alpha, beta, S0=None, cu_seqlens=None, scale=None) -> (o, S_T)`` -- the
+  gated delta rule; q, k may have fewer heads than v
+* ``decode_step_gdr(q, k, v, alpha, beta, S, slot_idx=None, scale=None, o=None) -> o`` (S updated
+  in place)
+* ``beam_select(logits, scores, done=None, end_token=0) -> (scores, token, parent, done)`` -- the W
+  best of W x V candidates of a beam search step
+* ``beam_reorder(parent, slot_idx, S, P=None) -> slot_idx`` of the new beams (S and P updated in
+  place)
 """
 
 from __future__ import annotations
@@ -96,6 +104,16 @@ def lib():
     L.kdn_backward_workspace_bytes.restype = sz
     L.kdn_forward_workspace_bytes.argtypes = [i32] * 7 + [ctypes.c_int, i32, i32]
     L.kdn_gain_workspace_bytes.argtypes = [i32] * 6
+    L.kdn_forward_gdr.argtypes = [vp] * 9 + [i32] * 7 + [ctypes.c_int, f32, vp, sz, vp]
+    L.kdn_forward_gdr_workspace_bytes.argtypes = [i32] * 7 + [ctypes.c_int, i32]
+    L.kdn_forward_gdr_workspace_bytes.restype = sz
+    L.kdn_decode_step_gdr.argtypes = [vp] * 8 + [i32] * 6 + [ctypes.c_int, f32, vp]
+    L.kdn_beam_select.argtypes = [vp] * 3 + [i32] * 3 + [ctypes.c_int, i32] + [vp] * 5 + [sz, vp]
+    L.kdn_beam_select_workspace_bytes.argtypes = [i32] * 3
+    L.kdn_beam_select_workspace_bytes.restype = sz
+    L.kdn_beam_reorder.argtypes = [vp] * 3 + [i32] * 3 + [vp, sz, vp, sz, vp]
+    for name in ("kdn_forward_gdr", "kdn_decode_step_gdr", "kdn_beam_select", "kdn_beam_reorder"):
+        getattr(L, name).restype = ctypes.c_int
     for name in ("kdn_forward_diag", "kdn_forward_iso", "kdn_forward_diag_noalloc",
                  "kdn_decode_step", "kdn_gain_diag", "kdn_gain_iso", "kdn_forward_layer",
                  "kdn_decode_step_layer", "kdn_backward"):
@@ -421,3 +439,149 @@ def forward_kam(q, k, v, alpha, omega, r, S0=None, P0=None, cu_seqlens=None, sca
                                scale, _stream(dev))
     _check(st, "kdn_forward_kam")
     return o, S_T, P_T
+
+
+def _dev_ptrs(dev, *ts):
+    """_ptrs of tensors that must all be on one GPU."""
+    for t in ts:
+        if t is not None and t.device != dev:
+            raise ValueError(f"all tensors of a call must be on {dev}, found one on {t.device}")
+    return _ptrs(*ts)
+
+
+def _shape(t, shape, name):
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
+
+
+def _gdr_heads(q, k, v, alpha, beta):
+    """Checks the shapes and types of one call's inputs ([.., Hk, dk], [.., H, dv], [.., H]);
+    returns (leading sizes, H, Hk, dk, dv)."""
+    *lead, Hk, dk = k.shape
+    H, dv = v.shape[-2:]
+    lead = tuple(lead)
+    if q.shape != k.shape or v.shape[:-2] != lead or Hk == 0 or H % Hk:
+        raise ValueError(f"q {tuple(q.shape)}, k {tuple(k.shape)} and v {tuple(v.shape)} do not "
+                         "belong together (key heads must divide value heads)")
+    if alpha.shape != lead + (H,) or beta.shape != lead + (H,):
+        raise ValueError(f"alpha {tuple(alpha.shape)} and beta {tuple(beta.shape)} must be "
+                         f"{lead + (H,)}")
+    if not (q.dtype == k.dtype == v.dtype == alpha.dtype == beta.dtype):
+        raise TypeError("q, k, v, alpha and beta must share one dtype")
+    return lead, H, Hk, dk, dv
+
+
+def _gdr_sequences(lead, H, dk, dv, S0, cu_seqlens):
+    """(N, B, T) of a batch, with its initial state and sequence table checked."""
+    if len(lead) != 2:
+        raise ValueError("q, k and v are [B, T, heads, d]")
+    B, T = lead
+    N = B
+    if cu_seqlens is not None:
+        if cu_seqlens.dtype != torch.int32:
+            raise TypeError("cu_seqlens must be int32")
+        N = cu_seqlens.numel() - 1
+    if S0 is not None:
+        _shape(_f32(S0), (N, H, dk, dv), "S0")
+    return N, B, T
+
+
+def forward_gdr(q, k, v, alpha, beta, S0=None, cu_seqlens=None, scale=None):
+    """Gated delta rule: S = alpha S + k u^T with u = beta (v - alpha S^T k), o = scale S^T q.
+    q, k [B,T,Hk,dk], v [B,T,H,dv], alpha, beta [B,T,H] of one dtype, Hk dividing H; returns
+    (o, S_T)."""
+    lead, H, Hk, dk, dv = _gdr_heads(q, k, v, alpha, beta)
+    N, B, T = _gdr_sequences(lead, H, dk, dv, S0, cu_seqlens)
+    dev, code = k.device, _dtype_code(k)
+    scale = float(dk ** -0.5 if scale is None else scale)
+    o = torch.empty(v.shape, dtype=v.dtype, device=dev)
+    S_T = torch.empty((N, H, dk, dv), dtype=torch.float32, device=dev)
+    ws_bytes = lib().kdn_forward_gdr_workspace_bytes(N, B, T, H, Hk, dk, dv, code,
+                                                     int(cu_seqlens is not None))
+    ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dev) if ws_bytes else None
+    ptrs = _dev_ptrs(dev, q, k, v, alpha, beta, S0, o, S_T, cu_seqlens)
+    st = lib().kdn_forward_gdr(*ptrs, N, B, T, H, Hk, dk, dv, code, scale, _ptr(ws), ws_bytes,
+                               _stream(dev))
+    if st != KDN_OK:
+        _check(st, "kdn_forward_gdr")
+    return o, S_T
+
+
+def decode_step_gdr(q, k, v, alpha, beta, S, slot_idx=None, scale=None, o=None):
+    """One token of the gated delta rule per row (q, k [R,Hk,dk], v [R,H,dv], alpha, beta [R,H]);
+    S [slots,H,dk,dv] updated in place; returns o."""
+    lead, H, Hk, dk, dv = _gdr_heads(q, k, v, alpha, beta)
+    if len(lead) != 1:
+        raise ValueError("q, k and v are [rows, heads, d]")
+    R = lead[0]
+    _shape(_f32(S), (S.shape[0], H, dk, dv), "S")
+    if slot_idx is not None:
+        if slot_idx.dtype != torch.int32:
+            raise TypeError("slot_idx must be int32")
+        _shape(slot_idx, lead, "slot_idx")
+    if o is None:
+        o = torch.empty(v.shape, dtype=v.dtype, device=v.device)
+    elif o.shape != v.shape or o.dtype != v.dtype:
+        raise ValueError("o must have the shape and dtype of v")
+    scale = float(dk ** -0.5 if scale is None else scale)
+    ptrs = _dev_ptrs(k.device, q, k, v, alpha, beta, S, slot_idx, o)
+    st = lib().kdn_decode_step_gdr(*ptrs, R, S.shape[0], H, Hk, dk, dv, _dtype_code(k), scale,
+                                   _stream(k.device))
+    if st != KDN_OK:
+        _check(st, "kdn_decode_step_gdr")
+    return o
+
+
+def beam_select(logits, scores, done=None, end_token=0):
+    """One selection step of beam search: logits [N,W,V] (bf16 or float32), scores [N,W] float32,
+    done [N,W] bool or None (finished beams, which go on with end_token at their own score).
+    Returns (scores [N,W] float32, token [N,W] int32, parent [N,W] int32, done [N,W] bool) of the W
+    best continuations, best first; equal ones in the order of beam, logit and token."""
+    if logits.dim() != 3:
+        raise ValueError("logits are [N, W, V]")
+    N, W, V = logits.shape
+    _shape(scores, (N, W), "scores")
+    if scores.dtype != torch.float32:
+        raise TypeError("scores must be float32")
+    if done is not None:
+        _shape(done, (N, W), "done")
+        if done.dtype != torch.bool:
+            raise TypeError("done must be bool")
+    dev = logits.device
+    scores_out = torch.empty((N, W), dtype=torch.float32, device=dev)
+    token, parent = torch.empty((2, N, W), dtype=torch.int32, device=dev).unbind(0)
+    done_out = torch.empty((N, W), dtype=torch.bool, device=dev)
+    ws_bytes = lib().kdn_beam_select_workspace_bytes(N, W, V)
+    ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dev) if ws_bytes else None
+    ptrs = _dev_ptrs(dev, logits, scores, done)
+    outs = _ptrs(scores_out, token, parent, done_out, ws)
+    st = lib().kdn_beam_select(*ptrs, N, W, V, _dtype_code(logits), int(end_token), *outs, ws_bytes,
+                               _stream(dev))
+    if st != KDN_OK:
+        _check(st, "kdn_beam_select")
+    return scores_out, token, parent, done_out
+
+
+def beam_reorder(parent, slot_idx, S, P=None):
+    """Moves the beams' states after a selection: parent, slot_idx [N,W] int32; S (and P) pools
+    whose first dimension is the slot, updated in place. A parent's first child keeps its slot,
+    every other child gets the slot of a beam without children and a copy of its parent's state.
+    Returns the new beams' slots [N,W]."""
+    if parent.dim() != 2:
+        raise ValueError("parent is [N, W]")
+    N, W = parent.shape
+    _shape(slot_idx, (N, W), "slot_idx")
+    if parent.dtype != torch.int32 or slot_idx.dtype != torch.int32:
+        raise TypeError("parent and slot_idx must be int32")
+    slots = S.shape[0]
+    if P is not None and P.shape[0] != slots:
+        raise ValueError("S and P must have the same number of slots")
+    out = torch.empty((N, W), dtype=torch.int32, device=parent.device)
+    ptrs = _dev_ptrs(parent.device, parent, slot_idx, out, S, P)
+    s_bytes = S.numel() // max(slots, 1) * S.element_size()
+    p_bytes = 0 if P is None else P.numel() // max(slots, 1) * P.element_size()
+    st = lib().kdn_beam_reorder(*ptrs[:3], N, W, slots, ptrs[3], s_bytes, ptrs[4], p_bytes,
+                                _stream(parent.device))
+    if st != KDN_OK:
+        _check(st, "kdn_beam_reorder")
+    return out
