@@ -24,4 +24,8 @@ hipError_t launch_gdr_decode(const void* q, const void* k, const void* v, const 
                              float scale, hipStream_t stream);
 hipError_t launch_gdr_recurrent(const GdrCall& c, hipStream_t stream);
 
+// Chunks of 64 tokens (kdn_gdr_chunk.hip).
+size_t gdr_chunk_workspace_bytes(bool packed, int N, int B, int T, int H, kdn_dtype_t dtype);
+hipError_t launch_gdr_chunked(const GdrCall& c, hipStream_t stream);
+
 }  // namespace kdn

@@ -21,6 +21,13 @@ kdn_status_t check_heads(int32_t H, int32_t Hk, int32_t dk, int32_t dv, kdn_dtyp
     return KDN_OK;
 }
 
+// Rows of a few tokens go token by token.
+bool gdr_short(int32_t B, int32_t T)
+{
+    (void)B;
+    return T <= 8;
+}
+
 }  // namespace
 
 extern "C" {
@@ -57,8 +64,10 @@ kdn_status_t kdn_decode_step_gdr(const void* q, const void* k, const void* v, co
 size_t kdn_forward_gdr_workspace_bytes(int32_t N, int32_t B, int32_t T, int32_t H, int32_t Hk,
                                        int32_t dk, int32_t dv, kdn_dtype_t dtype, int32_t packed)
 {
-    (void)N; (void)B; (void)T; (void)H; (void)Hk; (void)dk; (void)dv; (void)dtype; (void)packed;
-    return 0;
+    if (N <= 0 || B <= 0 || T <= 0 || H <= 0 || Hk <= 0 || H % Hk != 0 || !head_ok(dk) ||
+        !head_ok(dv) || (dtype != KDN_F32 && dtype != KDN_BF16) || gdr_short(B, T))
+        return 0;
+    return gdr_chunk_workspace_bytes(packed != 0, N, B, T, H, dtype);
 }
 
 kdn_status_t kdn_forward_gdr(const void* q, const void* k, const void* v, const void* alpha,
@@ -95,7 +104,9 @@ kdn_status_t kdn_forward_gdr(const void* q, const void* k, const void* v, const 
         return fail(KDN_ERR_INVALID_ARG, "the workspace overlaps an output");
     const GdrCall c = {q, k, v, alpha, beta, S0, o, S_T, {cu_seqlens, N, B, T, H}, Hk, dk, dv,
                        dtype, scale, workspace};
-    return hip_status(launch_gdr_recurrent(c, (hipStream_t)stream), "kdn_forward_gdr launch");
+    return hip_status(gdr_short(B, T) ? launch_gdr_recurrent(c, (hipStream_t)stream)
+                                      : launch_gdr_chunked(c, (hipStream_t)stream),
+                      "kdn_forward_gdr launch");
 }
 
 }  // extern "C"
