@@ -343,6 +343,29 @@ size_t kdn_forward_gdr_workspace_bytes(int32_t N, int32_t B, int32_t T, int32_t 
                                        int32_t dk, int32_t dv, kdn_dtype_t dtype, int32_t packed);
 
 /*
+ * Backward of kdn_forward_gdr: the gradients of a scalar loss with respect to every input, given those
+ * of its outputs, dO [B,T,H,dv] (dtype, NULL = 0) and dS_T [N,H,dk,dv] float32 (NULL = 0).
+ *   dq, dk [B,T,Hk,dk], dv [B,T,H,dv], dalpha, dbeta [B,T,H] in the call's dtype (computed in float32
+ *   and rounded once; dq and dk are the sums over the value heads of a key head); dS0 [N,H,dk,dv]
+ *   float32 or NULL. Fully overwritten for the tokens of the batch's sequences; no gradient may overlap
+ *   another or any other buffer of the call.
+ *   A gate of 0 counts as 2^-100, the least gate whose gradient is formed.
+ *   workspace: kdn_backward_gdr_workspace_bytes(...) bytes, 16-byte aligned, about 2.2 KB per token and
+ *   value head at dk = dv = 128 in bf16; no initialisation needed.
+ */
+kdn_status_t kdn_backward_gdr(const void* q, const void* k, const void* v, const void* alpha,
+                              const void* beta, const float* S0, const int32_t* cu_seqlens, int32_t N,
+                              int32_t B, int32_t T, int32_t H, int32_t Hk, int32_t dk, int32_t dv,
+                              kdn_dtype_t dtype, float scale, const void* dO, const float* dS_T,
+                              void* dq, void* dk_out, void* dv_out, void* dalpha, void* dbeta,
+                              float* dS0, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Device scratch (bytes) kdn_backward_gdr needs (packed != 0 with cu_seqlens); 0 for arguments it
+ * rejects.                                                                                     */
+size_t kdn_backward_gdr_workspace_bytes(int32_t N, int32_t B, int32_t T, int32_t H, int32_t Hk,
+                                        int32_t dk, int32_t dv, kdn_dtype_t dtype, int32_t packed);
+
+/*
  * One token of the gated delta rule per row, the state resident in a slot pool and updated in
  * place: q, k [R,Hk,dk]; v, o [R,H,dv]; alpha, beta [R,H] (dtype); S [num_slots,H,dk,dv] float32;
  * slot_idx as in kdn_decode_step (NULL: row i uses slot i; a row whose slot is negative or

@@ -28,4 +28,16 @@ hipError_t launch_gdr_recurrent(const GdrCall& c, hipStream_t stream);
 size_t gdr_chunk_workspace_bytes(bool packed, int N, int B, int T, int H, kdn_dtype_t dtype);
 hipError_t launch_gdr_chunked(const GdrCall& c, hipStream_t stream);
 
+// Backward (kdn_gdr_bwd.hip): fwd.o and fwd.S_T are not read. Gradients in the call's type, dS0 float32.
+struct GdrGradCall {
+    GdrCall fwd;
+    const void* dO;
+    const float* dS_T;
+    void *dq, *dk, *dv, *dalpha, *dbeta;
+    float* dS0;
+};
+size_t gdr_backward_workspace_bytes(bool packed, int N, int B, int T, int H, int dk, int dv,
+                                    kdn_dtype_t dtype);
+hipError_t launch_gdr_backward(const GdrGradCall& b, hipStream_t stream);
+
 }  // namespace kdn

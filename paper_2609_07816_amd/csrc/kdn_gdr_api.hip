@@ -100,6 +100,8 @@ kdn_status_t kdn_forward_gdr(const void* q, const void* k, const void* v, const 
     if (need > 0 && (!workspace || workspace_bytes < need))
         return fail(KDN_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need,
                     workspace ? workspace_bytes : (size_t)0);
+    if ((uintptr_t)workspace & 15)
+        return fail(KDN_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
     if (overlaps(workspace, workspace_bytes, o, nv) || overlaps(workspace, workspace_bytes, S_T, ns))
         return fail(KDN_ERR_INVALID_ARG, "the workspace overlaps an output");
     const GdrCall c = {q, k, v, alpha, beta, S0, o, S_T, {cu_seqlens, N, B, T, H}, Hk, dk, dv,
@@ -107,6 +109,61 @@ kdn_status_t kdn_forward_gdr(const void* q, const void* k, const void* v, const 
     return hip_status(gdr_short(B, T) ? launch_gdr_recurrent(c, (hipStream_t)stream)
                                       : launch_gdr_chunked(c, (hipStream_t)stream),
                       "kdn_forward_gdr launch");
+}
+
+size_t kdn_backward_gdr_workspace_bytes(int32_t N, int32_t B, int32_t T, int32_t H, int32_t Hk,
+                                        int32_t dk, int32_t dv, kdn_dtype_t dtype, int32_t packed)
+{
+    if (N <= 0 || B <= 0 || T <= 0 || H <= 0 || Hk <= 0 || H % Hk != 0 || !head_ok(dk) ||
+        !head_ok(dv) || (dtype != KDN_F32 && dtype != KDN_BF16))
+        return 0;
+    return gdr_backward_workspace_bytes(packed != 0, N, B, T, H, dk, dv, dtype);
+}
+
+kdn_status_t kdn_backward_gdr(const void* q, const void* k, const void* v, const void* alpha,
+                              const void* beta, const float* S0, const int32_t* cu_seqlens, int32_t N,
+                              int32_t B, int32_t T, int32_t H, int32_t Hk, int32_t dk, int32_t dv,
+                              kdn_dtype_t dtype, float scale, const void* dO, const float* dS_T,
+                              void* dq, void* dk_out, void* dv_out, void* dalpha, void* dbeta,
+                              float* dS0, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!q || !k || !v || !alpha || !beta)
+        return fail(KDN_ERR_INVALID_ARG, "null required input (q, k, v, alpha, beta)");
+    if (!dq || !dk_out || !dv_out || !dalpha || !dbeta)
+        return fail(KDN_ERR_INVALID_ARG, "null required gradient (dq, dk, dv, dalpha, dbeta)");
+    kdn_status_t st = check_heads(H, Hk, dk, dv, dtype, scale);
+    if (st == KDN_OK) st = check_seq(cu_seqlens, N, B, T, H);
+    if (st == KDN_OK)
+        st = check_aligned({{q, "q"}, {k, "k"}, {v, "v"}, {dO, "dO"}, {S0, "S0"}, {dS_T, "dS_T"},
+                            {dq, "dq"}, {dk_out, "dk"}, {dv_out, "dv"}, {dS0, "dS0"}});
+    if (st != KDN_OK) return st;
+    const size_t es = esize(dtype), rows = (size_t)B * T, ns = (size_t)N * H * dk * dv * 4;
+    const size_t nk = rows * Hk * dk * es, nv = rows * H * dv * es, ng = rows * H * es;
+    // every buffer the call reads or writes, with its extent; the gradients may overlap none
+    const void* bufs[10] = {q, k, v, alpha, beta, dO, S0, dS_T, cu_seqlens, workspace};
+    const size_t bsz[10] = {nk, nk, nv, ng, ng, nv, ns, ns, cu_seqlens ? (size_t)(N + 1) * 4 : 0,
+                            workspace_bytes};
+    const void* outs[6] = {dq, dk_out, dv_out, dalpha, dbeta, dS0};
+    const size_t osz[6] = {nk, nk, nv, ng, ng, ns};
+    for (int o = 0; o < 6; ++o) {
+        for (int i = 0; i < 10; ++i)
+            if (overlaps(outs[o], osz[o], bufs[i], bsz[i]))
+                return fail(KDN_ERR_INVALID_ARG, "gradient %d overlaps argument buffer %d", o, i);
+        for (int o2 = 0; o2 < o; ++o2)
+            if (overlaps(outs[o], osz[o], outs[o2], osz[o2]))
+                return fail(KDN_ERR_INVALID_ARG, "gradients %d and %d overlap", o2, o);
+    }
+    const size_t need = gdr_backward_workspace_bytes(cu_seqlens != nullptr, N, B, T, H, dk, dv, dtype);
+    if (!workspace || workspace_bytes < need)
+        return fail(KDN_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need,
+                    workspace ? workspace_bytes : (size_t)0);
+    if ((uintptr_t)workspace & 15)
+        return fail(KDN_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+    const GdrCall c = {q, k, v, alpha, beta, S0, nullptr, nullptr, {cu_seqlens, N, B, T, H}, Hk, dk, dv,
+                       dtype, scale, workspace};
+    return hip_status(launch_gdr_backward({c, dO, dS_T, dq, dk_out, dv_out, dalpha, dbeta, dS0},
+                                          (hipStream_t)stream),
+                      "kdn_backward_gdr launch");
 }
 
 }  // extern "C"

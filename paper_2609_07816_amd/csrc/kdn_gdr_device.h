@@ -157,31 +157,212 @@ __device__ __forceinline__ bool gdr_locate(const GdrSeq& s, int g, int& n, int& 
     return m >= 0 && c0 < c1;
 }
 
-// One chunk and head's record: per-token factors, then matrices in fragment order (f16). The strictly
-// lower triangular matrices keep the six fragments that hold it: (row block b, columns 32 s ..) with
-// s <= b / 2.
+// One chunk and head's record: per-token factors, then matrices in fragment order (f16, halves hi and
+// lo). A strictly lower triangular matrix keeps the six fragments that hold it: (row block b, columns
+// 32 s ..) with s <= b / 2; a transposed one those with s >= b / 2.
 enum GdrFactor {
     F_KS,   // power of two that scales k's row
     F_QS,   // the same for q
     F_G1,   // decay since the chunk's start, over k's scale
     F_BE,   // beta
-    F_NR,   // inverse scale of N's row
+    F_WR,   // inverse scale of W's row
     F_W,    // decay to the chunk's end, over k's scale
     F_GQ,   // decay since the chunk's start times the output scale, over q's scale
     F_AR,   // output scale times the inverse scale of A's row
-    F_COUNT
+    F_WTR,  // the same of the transposed matrices (backward)
+    F_ATR,
+    F_L,    // float64 cumulative log2 decay (two rows)
+    F_COUNT = F_L + 2
 };
-constexpr int REC_FACTORS = F_COUNT * GC;          // floats; then the chunk's whole decay
-constexpr int REC_HEAD = (REC_FACTORS + 64) * 4;   // bytes
-constexpr int TRI = 6;                             // fragments of a lower triangular matrix
+constexpr int REC_FACTORS = F_COUNT * GC;         // floats; then the chunk's whole decay
+constexpr int REC_HEAD = (REC_FACTORS + 64) * 4;  // bytes
+constexpr int TRI = 6;                            // fragments of a triangular matrix
 constexpr int TRI_BYTES = TRI * 1024;
 __device__ __forceinline__ int tri_frag(int b, int s) { return b < 2 ? b : 2 * b - 2 + s; }
+__device__ __forceinline__ int tri_frag_t(int b, int s) { return b < 2 ? 2 * b + s : b + 2; }
 
-// N hi, N lo, A hi (, A lo)
 template <class T> constexpr int gdr_parts() { return sizeof(T) == 4 ? 2 : 1; }
-template <class T> constexpr size_t gdr_rec_bytes()
+
+// Records of the forward (W hi, W lo, A hi (, A lo)) and of the backward (W, W^T, A^T, hi and lo).
+template <class T, bool BWD> constexpr int gdr_rec_bytes()
 {
-    return REC_HEAD + (size_t)(2 + gdr_parts<T>()) * TRI_BYTES;
+    return REC_HEAD + (BWD ? 6 : 2 + gdr_parts<T>()) * TRI_BYTES;
 }
+
+template <class T>
+struct ChunkArgs {
+    const T *q, *k, *v, *alpha, *beta;
+    const float* S0;
+    T* o;
+    float* S_T;
+    GdrSeq seq;
+    int H, Hk, rep, maxch;
+    float scale;
+    char* rec;
+};
+
+__device__ __forceinline__ float4 ld4(const float* p) { return *reinterpret_cast<const float4*>(p); }
+
+__device__ __forceinline__ half8 frag_ld(const char* base, int frag, int lane)
+{
+    return *reinterpret_cast<const half8*>(base + frag * 1024 + lane * 16);
+}
+
+// LDS of one chunk: fragment-order K, K transposed, Q, Q transposed (each if wanted, P parts), then the
+// record's head and the part of its matrices that the kernel uses.
+template <class T, int DK, bool KR, bool KC, bool QR, bool QC, int MATS>
+struct ChunkLds {
+    static constexpr int P = gdr_parts<T>();
+    static constexpr int KSTEPS = DK < 32 ? 1 : DK / 32;
+    static constexpr int KT = DK / 16;
+    static constexpr int RB = 4 * KSTEPS * 1024;  // K or Q by rows, one part
+    static constexpr int CB = KT * 2 * 1024;      // transposed, one part
+    static constexpr int O_K = 0;
+    static constexpr int O_KT = O_K + (KR ? P * RB : 0);
+    static constexpr int O_Q = O_KT + (KC ? P * CB : 0);
+    static constexpr int O_QT = O_Q + (QR ? P * RB : 0);
+    static constexpr int O_REC = O_QT + (QC ? P * CB : 0);
+    static constexpr int REC = MATS < 0 ? 0 : REC_HEAD + MATS * TRI_BYTES;
+    static constexpr int BYTES = O_REC + REC;
+    static constexpr int NBUF = 2 * BYTES <= 160 * 1024 ? 2 : 1;
+    static constexpr bool kr = KR, kc = KC, qr = QR, qc = QC;
+};
+
+// Four tokens x eight channels of K or Q as stored.
+template <class T>
+struct Raw8 {
+    uint4 x[4][sizeof(T) / 2];
+
+    __device__ __forceinline__ void load(const T* base, size_t step, int t, int len, bool on)
+    {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int u = 0; u < (int)sizeof(T) / 2; ++u) {
+                x[r][u] = make_uint4(0, 0, 0, 0);
+                if (on && t + r < len)
+                    x[r][u] = reinterpret_cast<const uint4*>(base + (size_t)(t + r) * step)[u];
+            }
+    }
+    __device__ __forceinline__ float value(int r, int e) const
+    {
+        const uint4& y = x[r][e / (16 / (int)sizeof(T))];
+        const unsigned z[4] = {y.x, y.y, y.z, y.w};
+        if constexpr (sizeof(T) == 4) {
+            return __uint_as_float(z[e & 3]);
+        } else {
+            const unsigned p = z[e / 2];
+            return __uint_as_float(e & 1 ? p & 0xFFFF0000u : p << 16);
+        }
+    }
+    // Scaled by row, part p (0: hi, 1: lo), to the row fragments and the transposed ones.
+    template <bool ROWS, bool COLS, int KSTEPS>
+    __device__ __forceinline__ void store(const float4& sc, int p, int t, int c, _Float16* rows,
+                                          _Float16* cols) const
+    {
+        const float f[4] = {sc.x, sc.y, sc.z, sc.w};
+        _Float16 y[4][8];
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float z = value(r, e) * f[r];
+                y[r][e] = (_Float16)z;
+                if (p == 1) y[r][e] = (_Float16)(z - (float)y[r][e]);
+            }
+        if (ROWS)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+                    *reinterpret_cast<half4*>(rows + frag_at(t + r, c + 4 * u, KSTEPS)) =
+                        half4{y[r][4 * u], y[r][4 * u + 1], y[r][4 * u + 2], y[r][4 * u + 3]};
+        if (COLS)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                *reinterpret_cast<half4*>(cols + frag_at(c + e, t, 2)) =
+                    half4{y[0][e], y[1][e], y[2][e], y[3][e]};
+    }
+};
+
+// The loading side of a workgroup: NT threads bring a chunk from memory to registers, and from there
+// to LDS. SKIP: bytes of the record between its head and the matrices wanted.
+template <class T, int DK, class Lds, int NT, int SKIP>
+struct Loader {
+    static constexpr int TASKS = 2 * DK;  // (4 tokens, 8 channels) pieces of K, or of Q
+    static constexpr int TPT = (TASKS + NT - 1) / NT;
+    static constexpr int RECP = (Lds::REC / 16 + NT - 1) / NT;
+    static constexpr bool useq = Lds::qr || Lds::qc;
+    Raw8<T> k[TPT], q[useq ? TPT : 1];
+    float4 ks[TPT], qs[useq ? TPT : 1];  // the rows' scales
+    uint4 rec[RECP > 0 ? RECP : 1];
+
+    __device__ __forceinline__ void load(const T* kbase, const T* qbase, size_t step, int tid, int len,
+                                         const char* recp)
+    {
+#pragma unroll
+        for (int j = 0; j < TPT; ++j) {
+            const int task = tid + NT * j, t = 4 * (task / (DK / 8) % 16), c = 8 * (task % (DK / 8));
+            const bool on = TASKS % NT == 0 || task < TASKS;
+            const float* fac = reinterpret_cast<const float*>(recp);
+            ks[j] = ld4(fac + F_KS * GC + t);
+            k[j].load(kbase + c, step, t, len, on);
+            if (useq) {
+                qs[j] = ld4(fac + F_QS * GC + t);
+                q[j].load(qbase + c, step, t, len, on);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < RECP; ++j) {
+            const int at = tid + NT * j;
+            if (at < Lds::REC / 16)
+                rec[j] = reinterpret_cast<const uint4*>(
+                    recp + (at < REC_HEAD / 16 ? 0 : SKIP))[at];
+        }
+    }
+
+    __device__ __forceinline__ void store(char* buf, int tid)
+    {
+#pragma unroll
+        for (int j = 0; j < TPT; ++j) {
+            const int task = tid + NT * j, t = 4 * (task / (DK / 8)), c = 8 * (task % (DK / 8));
+            if (TASKS % NT != 0 && task >= TASKS) break;
+#pragma unroll
+            for (int p = 0; p < Lds::P; ++p) {
+                k[j].template store<Lds::kr, Lds::kc, Lds::KSTEPS>(
+                    ks[j], p, t, c, reinterpret_cast<_Float16*>(buf + Lds::O_K + p * Lds::RB),
+                    reinterpret_cast<_Float16*>(buf + Lds::O_KT + p * Lds::CB));
+                if (useq)
+                    q[j].template store<Lds::qr, Lds::qc, Lds::KSTEPS>(
+                        qs[j], p, t, c, reinterpret_cast<_Float16*>(buf + Lds::O_Q + p * Lds::RB),
+                        reinterpret_cast<_Float16*>(buf + Lds::O_QT + p * Lds::CB));
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < RECP; ++j)
+            if (tid + NT * j < Lds::REC / 16)
+                reinterpret_cast<uint4*>(buf + Lds::O_REC)[tid + NT * j] = rec[j];
+    }
+};
+
+// Column of 16 values x four row blocks of [tokens][H][DV] in the layout of result tiles, as stored.
+template <class T>
+__device__ __forceinline__ void load_tile(const T* p, size_t step, int gq, int len, T* x)
+{
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            x[4 * b + r] = p[(size_t)min(16 * b + 4 * gq + r, len - 1) * step];
+}
+
+__device__ __forceinline__ void unpack4(const float4& x, float* y)
+{
+    y[0] = x.x; y[1] = x.y; y[2] = x.z; y[3] = x.w;
+}
+
+// Launchers of the kernels that forward and backward share (kdn_gdr_prep.hip).
+template <class T>
+hipError_t launch_gdr_prep(const ChunkArgs<T>& a, int dk, bool backward, hipStream_t stream);
 
 }  // namespace kdn

@@ -1,0 +1,296 @@
+// Gated delta rule over chunks of 64 tokens on gfx950: each chunk's matrices, for the forward and the
+// backward.
+//
+// With l_t the cumulative log2 decay inside a chunk and R_ts = 2^(l_t - l_s) for s <= t:
+//   M = tril(R (K K^T), -1), A = tril(R (Q K^T)), W = (I + M beta)^-1 M
+// so that the innovations are E = X - W (beta X) for X = V - 2^l K S, the writes U = beta E, and the
+// adjoint of the writes solves as Y = D - W^T (beta D). W needs no division by beta, which may be 0.
+#include "kdn_gdr_device.h"
+
+namespace kdn {
+namespace {
+
+// ------------------------------------------------------------------------------------------
+// gdr_prep: wave w has rows 16w .. 16w+15 of the chunk. Products of the inputs as they are stored
+// (bf16 or float32 instructions, exact operands), the decay ratios from float64 cumulative logarithms
+// (a difference of two sums has the error of the difference), the solve in float32: in the diagonal
+// 16 x 16 blocks by substitution (lane = column: T_bb = (I + M_bb beta)^-1 in one row of 16 lanes,
+// W_bb = T_bb M_bb in another), the others by block products
+// W_bc = T_bb (M_bc - sum_m M_bm beta_m W_mc), wave = block column.
+// ------------------------------------------------------------------------------------------
+constexpr int LP = 20;  // floats of a tile's row in LDS
+constexpr int MP = 68;  // floats of a matrix row in LDS
+
+template <class T, int DK, bool BWD>
+__global__ __launch_bounds__(256) void gdr_prep_kernel(const ChunkArgs<T> a)
+{
+    using Fr = Frag<T, DK>;
+    using V = typename Fr::V;
+    __shared__ __align__(16) float sL[6][16 * LP];  // M's blocks below the diagonal ones: (b, c) at
+                                                    // b (b - 1) / 2 + c
+    __shared__ __align__(16) float sD[4][16 * LP];  // the diagonal blocks, then T_bb
+    __shared__ __align__(16) float sM[GC * MP];     // A, then W
+    __shared__ double s_l[GC];
+    __shared__ __align__(16) float s_be[GC];
+    const int g = blockIdx.x / a.H, h = blockIdx.x % a.H;
+    int n, c0, c1;
+    if (!gdr_locate(a.seq, g, n, c0, c1)) return;  // uniform across the workgroup
+    const int len = c1 - c0;
+    const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, gq = lane >> 4, li = lane & 15;
+    const int hk = h / a.rep;
+
+    // cumulative decays: lane = token, in every wave (the values of tokens past the end change nothing)
+    double l = 0.0;
+    float be = 0.f;
+    if (lane < len) {
+        const size_t at = (size_t)(c0 + lane) * a.H + h;
+        // a gate of 0 counts as 2^-100: what it lets through is lost against anything beside it
+        l = log2((double)fmaxf(to_f32(a.alpha[at]), 0x1p-100f));
+        be = to_f32(a.beta[at]);
+    }
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const double y = __shfl_up(l, off, 64);
+        if (lane >= off) l += y;
+    }
+    if (w == 0) {
+        s_l[lane] = l;
+        s_be[lane] = be;
+    }
+    const double l_end = __shfl(l, 63, 64);
+
+    // operands: this wave's rows of K and Q
+    const T* kbase = a.k + ((size_t)c0 * a.Hk + hk) * DK + gq * (Fr::KF / 4);
+    const T* qbase = a.q + ((size_t)c0 * a.Hk + hk) * DK + gq * (Fr::KF / 4);
+    const size_t step = (size_t)a.Hk * DK;
+    auto load_rows = [&](const T* base, int b, V* f) {
+        const int t = 16 * b + li;
+#pragma unroll
+        for (int s = 0; s < Fr::NS; ++s) {
+            f[s] = V{};
+            if (t < len) f[s] = Fr::ld(base + t * step + s * Fr::KF);
+        }
+    };
+    V fk[Fr::NS], fq[Fr::NS];
+    load_rows(kbase, w, fk);
+    load_rows(qbase, w, fq);
+    // power-of-two scales of the rows
+    float mk = 0.f, mq = 0.f;
+#pragma unroll
+    for (int s = 0; s < Fr::NS; ++s) {
+        constexpr int E = Fr::KF / 4;
+        T x[E], y[E];
+        __builtin_memcpy(x, &fk[s], sizeof(V));
+        __builtin_memcpy(y, &fq[s], sizeof(V));
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            mk = fmaxf(mk, fabsf(to_f32(x[e])));
+            mq = fmaxf(mq, fabsf(to_f32(y[e])));
+        }
+    }
+    mk = column_max(mk);
+    mq = column_max(mq);
+    __syncthreads();
+
+    // products with the blocks c <= w; result lane (gq, li): rows 16w + 4gq + r, column 16c + li
+    double lr[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) lr[r] = s_l[16 * w + 4 * gq + r];
+    for (int c = 0; c < 4; ++c) {
+        float* am = sM + 16 * c + li;
+        if (c > w) {  // above the diagonal
+#pragma unroll
+            for (int r = 0; r < 4; ++r) am[(16 * w + 4 * gq + r) * MP] = 0.f;
+            continue;
+        }
+        V fc[Fr::NS];
+        load_rows(kbase, c, fc);
+        floatx4 kk = zero4(), qk = zero4();
+#pragma unroll
+        for (int s = 0; s < Fr::NS; ++s) {
+            kk = Fr::mma(kk, fk[s], fc[s]);
+            qk = Fr::mma(qk, fq[s], fc[s]);
+        }
+        const double ls = s_l[16 * c + li];
+        float* lt = c == w ? sD[w] : sL[w * (w - 1) / 2 + c];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int t = 16 * w + 4 * gq + r, s = 16 * c + li;
+            const float rho = t >= s ? __builtin_amdgcn_exp2f((float)(lr[r] - ls)) : 0.f;
+            lt[(4 * gq + r) * LP + li] = t > s ? rho * kk[r] : 0.f;
+            am[t * MP] = t >= s ? rho * qk[r] : 0.f;
+        }
+    }
+    wave_lds_fence();
+    // this wave's diagonal block by substitution, column li: of the identity in the lanes gq = 0, of M
+    // in the others; z_j = beta_j x_j
+    float z[16], rhs[16], x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) rhs[i] = gq == 0 ? (i == li ? 1.f : 0.f) : sD[w][i * LP + li];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        float y = rhs[i];
+#pragma unroll
+        for (int j4 = 0; j4 < i; j4 += 4) {
+            const float4 row = ld4(sD[w] + i * LP + j4);
+            y = fmaf(-row.x, z[j4], y);
+            if (j4 + 1 < i) y = fmaf(-row.y, z[j4 + 1], y);
+            if (j4 + 2 < i) y = fmaf(-row.z, z[j4 + 2], y);
+            if (j4 + 3 < i) y = fmaf(-row.w, z[j4 + 3], y);
+        }
+        x[i] = y;
+        z[i] = y * s_be[16 * w + i];
+    }
+    wave_lds_fence();
+    if (gq == 0)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sD[w][i * LP + li] = x[i];
+    __syncthreads();
+
+    // A's rows to the record: thread = (row, 16 columns)
+    char* rec = a.rec + ((size_t)g * a.H + h) * gdr_rec_bytes<T, BWD>();
+    float* fac = reinterpret_cast<float*>(rec);
+    _Float16* frag = reinterpret_cast<_Float16*>(rec + REC_HEAD);
+    const int row = tid >> 2, quarter = tid & 3;
+    // a row (TR: a column) of sM in halves; returns its inverse scale
+    auto write_rows = [&](auto transposed, _Float16* hi, _Float16* lo) -> float {
+        constexpr bool TR = decltype(transposed)::value;
+        float4 y[4];
+        float m = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int c = 16 * quarter + 4 * j;
+            if constexpr (TR)
+                y[j] = make_float4(sM[c * MP + row], sM[(c + 1) * MP + row], sM[(c + 2) * MP + row],
+                                   sM[(c + 3) * MP + row]);
+            else
+                y[j] = ld4(sM + row * MP + c);
+            m = fmaxf(m, fmaxf(fmaxf(fabsf(y[j].x), fabsf(y[j].y)), fmaxf(fabsf(y[j].z), fabsf(y[j].w))));
+        }
+        m = fmaxf(m, __shfl_xor(m, 1, 64));
+        m = fmaxf(m, __shfl_xor(m, 2, 64));
+        float sc, inv;
+        pow2_scale(m, sc, inv);
+        const int b = row >> 4, s = quarter / 2;
+        if (TR ? s >= b / 2 : s <= b / 2) {
+            _Float16* at = hi + (TR ? tri_frag_t(b, s) : tri_frag(b, s)) * 512 + (row & 15) * 8 +
+                           (quarter & 1) * 4;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float z[4] = {y[j].x * sc, y[j].y * sc, y[j].z * sc, y[j].w * sc};
+                half4 p, q;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    p[e] = (_Float16)z[e];
+                    q[e] = (_Float16)(z[e] - (float)p[e]);
+                }
+                *reinterpret_cast<half4*>(at + 16 * 8 * j) = p;
+                if (lo) *reinterpret_cast<half4*>(lo + (at - hi) + 16 * 8 * j) = q;
+            }
+        }
+        return inv;
+    };
+    using Rows = std::integral_constant<bool, false>;
+    using Cols = std::integral_constant<bool, true>;
+    constexpr int NH = TRI * 512;  // values of a triangular matrix
+    float a_inv;
+    if constexpr (BWD)
+        a_inv = write_rows(Cols{}, frag + 4 * NH, frag + 5 * NH);
+    else
+        a_inv = write_rows(Rows{}, frag + 2 * NH, gdr_parts<T>() == 2 ? frag + 3 * NH : nullptr);
+    __syncthreads();  // sM is read
+
+    // block column w of W: W_ww, then W_bw for b > w. A result tile is the B operand of the next product.
+    if (gq == 1)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sM[(16 * w + i) * MP + 16 * w + li] = x[i];
+    for (int b = 0; b < w; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sM[(16 * b + 4 * gq + r) * MP + 16 * w + li] = 0.f;
+    wave_lds_fence();
+    {
+        floatx4 t[4];  // beta W_bw
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int i = 16 * w + 4 * gq + r;
+            t[0][r] = s_be[i] * sM[i * MP + 16 * w + li];
+        }
+#pragma unroll
+        for (int d = 1; d < 4; ++d) {
+            const int b = w + d;
+            if (b < 4) {
+                floatx4 y = zero4();
+#pragma unroll
+                for (int m = 0; m < d; ++m)
+                    y = mma16_f32(y, ld4(sL[b * (b - 1) / 2 + w + m] + li * LP + 4 * gq), t[m]);
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    y[r] = sL[b * (b - 1) / 2 + w][(4 * gq + r) * LP + li] - y[r];
+                y = mma16_f32(zero4(), ld4(sD[b] + li * LP + 4 * gq), y);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int i = 16 * b + 4 * gq + r;
+                    sM[i * MP + 16 * w + li] = y[r];
+                    t[d][r] = s_be[i] * y[r];
+                }
+            }
+        }
+    }
+    __syncthreads();
+    const float w_inv = write_rows(Rows{}, frag, frag + NH);
+
+    // factors
+    if (quarter == 0) {
+        fac[(BWD ? F_ATR : F_AR) * GC + row] = a.scale * a_inv;
+        fac[F_WR * GC + row] = w_inv;
+        fac[F_BE * GC + row] = s_be[row];
+    }
+    if constexpr (BWD) {
+        const float inv = write_rows(Cols{}, frag + 2 * NH, frag + 3 * NH);
+        if (quarter == 0) fac[F_WTR * GC + row] = inv;
+        if (w == 0) reinterpret_cast<double*>(fac + F_L * GC)[lane] = l;
+    }
+    if (gq == 0) {
+        const int t = 16 * w + li;
+        float ks, ki, qs, qi;
+        pow2_scale(mk, ks, ki);
+        pow2_scale(mq, qs, qi);
+        const float dec = __builtin_amdgcn_exp2f((float)s_l[t]);
+        fac[F_KS * GC + t] = ks;
+        fac[F_QS * GC + t] = qs;
+        fac[F_G1 * GC + t] = dec * ki;
+        fac[F_W * GC + t] = __builtin_amdgcn_exp2f((float)(l_end - s_l[t])) * ki;
+        fac[F_GQ * GC + t] = dec * a.scale * qi;
+        if (t == 0) fac[REC_FACTORS] = __builtin_amdgcn_exp2f((float)l_end);
+    }
+}
+
+template <class T, int DK>
+hipError_t launch_dk(const ChunkArgs<T>& a, bool backward, hipStream_t stream)
+{
+    const dim3 grid((unsigned)(a.maxch * a.H)), block(256);
+    if (backward)
+        hipLaunchKernelGGL((gdr_prep_kernel<T, DK, true>), grid, block, 0, stream, a);
+    else
+        hipLaunchKernelGGL((gdr_prep_kernel<T, DK, false>), grid, block, 0, stream, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+template <class T>
+hipError_t launch_gdr_prep(const ChunkArgs<T>& a, int dk, bool backward, hipStream_t stream)
+{
+    switch (dk) {
+    case 16: return launch_dk<T, 16>(a, backward, stream);
+    case 32: return launch_dk<T, 32>(a, backward, stream);
+    case 64: return launch_dk<T, 64>(a, backward, stream);
+    case 128: return launch_dk<T, 128>(a, backward, stream);
+    }
+    return hipErrorInvalidValue;
+}
+
+template hipError_t launch_gdr_prep<float>(const ChunkArgs<float>&, int, bool, hipStream_t);
+template hipError_t launch_gdr_prep<bf16>(const ChunkArgs<bf16>&, int, bool, hipStream_t);
+
+}  // namespace kdn

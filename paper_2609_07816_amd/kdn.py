@@ -24,6 +24,8 @@ Functions mirror the C entry points:
   -> (o, S_T, P_T)`` -- the dense-covariance Kalman Associative Memory
 * ``forward_gdr(q, k, v, alpha, beta, S0=None, cu_seqlens=None, scale=None) -> (o, S_T)`` -- the
   gated delta rule; q, k may have fewer heads than v
+* ``backward_gdr(q, k, v, alpha, beta, S0=None, cu_seqlens=None, scale=None, dO=None, dS_T=None)
+  -> dict`` of gradients in the inputs' types
 * ``decode_step_gdr(q, k, v, alpha, beta, S, slot_idx=None, scale=None, o=None) -> o`` (S updated
   in place)
 * ``beam_select(logits, scores, done=None, end_token=0) -> (scores, token, parent, done)`` -- the W
@@ -107,12 +109,16 @@ def lib():
     L.kdn_forward_gdr.argtypes = [vp] * 9 + [i32] * 7 + [ctypes.c_int, f32, vp, sz, vp]
     L.kdn_forward_gdr_workspace_bytes.argtypes = [i32] * 7 + [ctypes.c_int, i32]
     L.kdn_forward_gdr_workspace_bytes.restype = sz
+    L.kdn_backward_gdr.argtypes = ([vp] * 7 + [i32] * 7 + [ctypes.c_int, f32] + [vp] * 8 +
+                                   [vp, sz, vp])
+    L.kdn_backward_gdr_workspace_bytes.argtypes = [i32] * 7 + [ctypes.c_int, i32]
+    L.kdn_backward_gdr_workspace_bytes.restype = sz
     L.kdn_decode_step_gdr.argtypes = [vp] * 8 + [i32] * 6 + [ctypes.c_int, f32, vp]
     L.kdn_beam_select.argtypes = [vp] * 3 + [i32] * 3 + [ctypes.c_int, i32] + [vp] * 5 + [sz, vp]
     L.kdn_beam_select_workspace_bytes.argtypes = [i32] * 3
     L.kdn_beam_select_workspace_bytes.restype = sz
     L.kdn_beam_reorder.argtypes = [vp] * 3 + [i32] * 3 + [vp, sz, vp, sz, vp]
-    for name in ("kdn_forward_gdr", "kdn_decode_step_gdr", "kdn_beam_select", "kdn_beam_reorder"):
+    for name in ("kdn_forward_gdr", "kdn_backward_gdr", "kdn_decode_step_gdr", "kdn_beam_select", "kdn_beam_reorder"):
         getattr(L, name).restype = ctypes.c_int
     for name in ("kdn_forward_diag", "kdn_forward_iso", "kdn_forward_diag_noalloc",
                  "kdn_decode_step", "kdn_gain_diag", "kdn_gain_iso", "kdn_forward_layer",
@@ -505,6 +511,33 @@ def forward_gdr(q, k, v, alpha, beta, S0=None, cu_seqlens=None, scale=None):
     if st != KDN_OK:
         _check(st, "kdn_forward_gdr")
     return o, S_T
+
+
+def backward_gdr(q, k, v, alpha, beta, S0=None, cu_seqlens=None, scale=None, dO=None, dS_T=None):
+    """Gradients of a loss through forward_gdr, given its gradients dO (input dtype) and dS_T
+    (float32); None = zero. Returns a dict of dq, dk, dv, dalpha, dbeta in the inputs' dtype and dS0
+    in float32."""
+    lead, H, Hk, dk, dv = _gdr_heads(q, k, v, alpha, beta)
+    N, B, T = _gdr_sequences(lead, H, dk, dv, S0, cu_seqlens)
+    dev, code = k.device, _dtype_code(k)
+    if dO is not None and (dO.shape != v.shape or dO.dtype != v.dtype):
+        raise ValueError("dO must have the shape and dtype of v")
+    if dS_T is not None:
+        _shape(_f32(dS_T), (N, H, dk, dv), "dS_T")
+    scale = float(dk ** -0.5 if scale is None else scale)
+    g = dict(dq=torch.empty_like(q), dk=torch.empty_like(k), dv=torch.empty_like(v),
+             dalpha=torch.empty_like(alpha), dbeta=torch.empty_like(beta),
+             dS0=torch.empty((N, H, dk, dv), dtype=torch.float32, device=dev))
+    ws_bytes = lib().kdn_backward_gdr_workspace_bytes(N, B, T, H, Hk, dk, dv, code,
+                                                      int(cu_seqlens is not None))
+    ws = torch.empty(max(ws_bytes, 1), dtype=torch.uint8, device=dev)
+    ins = _dev_ptrs(dev, q, k, v, alpha, beta, S0, cu_seqlens)
+    outs = _dev_ptrs(dev, dO, dS_T, *g.values())
+    st = lib().kdn_backward_gdr(*ins, N, B, T, H, Hk, dk, dv, code, scale, *outs, _ptr(ws), ws_bytes,
+                                _stream(dev))
+    if st != KDN_OK:
+        _check(st, "kdn_backward_gdr")
+    return g
 
 
 def decode_step_gdr(q, k, v, alpha, beta, S, slot_idx=None, scale=None, o=None):

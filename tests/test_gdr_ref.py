@@ -85,6 +85,20 @@ def test_gdr_argument_errors(L):
     base = 0x7000000
     assert fwd(L, S0=ctypes.c_void_p(base), S_T=ctypes.c_void_p(base + 64)) == bad
     assert fwd(L, S_T=p[1]) == bad
+    g = [P(i) for i in range(10, 16)]
+
+    def bwd(ins=p[:5], S0=None, dO=P(6), dST=None, outs=g, ws=P(40), n=1 << 40, H=2, Hk=1, dk=64):
+        return L.kdn_backward_gdr(*ins, S0, None, 1, 1, 8, H, Hk, dk, 64, 1, F(1.0), dO, dST, *outs,
+                                  ws, n, None)
+
+    need = L.kdn_backward_gdr_workspace_bytes(1, 1, 8, 2, 1, 64, 64, 1, 0)
+    assert need > 0 and L.kdn_backward_gdr_workspace_bytes(1, 1, 8, 3, 2, 64, 64, 1, 0) == 0
+    assert bwd(ins=[None] + p[1:5]) == bad
+    assert bwd(outs=g[:3] + [None] + g[4:]) == bad
+    assert bwd(outs=[P(0)] + g[1:]) == bad and bwd(outs=[g[1]] + g[1:]) == bad
+    assert bwd(dO=P(12)) == bad                                  # dO is dv
+    assert bwd(Hk=3) == bad and bwd(dk=8) == kdn.KDN_ERR_UNSUPPORTED
+    assert bwd(n=need - 1) == kdn.KDN_ERR_WORKSPACE and bwd(ws=None) == kdn.KDN_ERR_WORKSPACE
     dec = [P(i) for i in range(5)]
 
     def step(ptrs=dec, S=P(8), slot=None, o=P(9), R=4, slots=4, H=2, Hk=1, dk=64, dv=64):
