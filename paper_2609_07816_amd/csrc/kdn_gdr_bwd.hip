@@ -36,11 +36,11 @@ struct GradArgs {
 template <class T, int DK, int DV, int NCW, int NLW>
 __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_reverse_kernel(const GradArgs<T> ga)
 {
-    using Sh = ChunkLds<T, DK, true, true, false, true, 4>;
+    using Sh = ChunkLds<T, DK, true, 4>;
+    constexpr int P = Sh::P, KS = Sh::KSTEPS, KT = Sh::KT;
     const ChunkArgs<T>& a = ga.c;
     constexpr int REC = gdr_rec_bytes<T, true>();
     constexpr int TILES = DV / (16 * NCW);
-    constexpr int DVP = DV < 32 ? 32 : DV;
     __shared__ __align__(16) char lds[Sh::NBUF * Sh::BYTES];
     const int chains = a.seq.N * a.H;
     const int chain = blockIdx.x / (8 * TILES) * 8 + blockIdx.x % 8, tile = blockIdx.x / 8 % TILES;
@@ -63,11 +63,11 @@ __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_reverse_kernel(const Gra
     if (wave >= NCW) {
         const int tid = threadIdx.x - 64 * NCW;
         Loader<T, DK, Sh, 64 * NLW, 2 * TRI_BYTES> ld;
-        const size_t step = (size_t)a.Hk * DK;
         auto load = [&](int i) {
             const int c = nch - 1 - i;
             const size_t at = ((size_t)(t0 + c * GC) * a.Hk + hk) * DK;
-            ld.load(a.k + at, a.q + at, step, tid, t1 - t0 - c * GC, rec0 + (size_t)c * rstep);
+            ld.load(a.k + at, a.q + at, (unsigned)(a.Hk * DK * sizeof(T)), tid,
+                    min(GC, t1 - t0 - c * GC), rec0 + (size_t)c * rstep);
         };
         if (nch > 0) {
             load(0);
@@ -86,26 +86,40 @@ __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_reverse_kernel(const Gra
         return;
     }
 
-    const int col = (tile * NCW + wave) * 16 + li;
+    const int ctile = tile * NCW + wave, col = ctile * 16 + li;
     const size_t sbase = ((size_t)n * a.H + h) * DK * DV + (size_t)(4 * gq) * DV + col;
-    floatx4 dS[Sh::KT];
+    const unsigned vstep = (unsigned)(a.H * DV * sizeof(T)), vcol = (unsigned)((h * DV + col) * sizeof(T));
+    auto vrow = [&](auto* p, int c) { return p + (size_t)(t0 + c * GC) * a.H * DV; };
+    unsigned off[16];
+    typename Raw1<T>::type on[16];
 #pragma unroll
-    for (int k = 0; k < Sh::KT; ++k)
+    for (int i = 0; i < 16; ++i) on[i] = 0;
+    floatx4 dS[KT];  // scaled by sS
+    ColScale sS = {1.f, 1.f}, sU = {1.f, 1.f};
+    const LaneOffsets lo(lane);
+    {
+        float m = 0.f;
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-            dS[k][r] = ga.dS_T ? ga.dS_T[sbase + (size_t)(16 * k + r) * DV] : 0.f;
-
-    const size_t vstep = (size_t)a.H * DV;
-    T on[16];
-    auto load_o = [&](int c) {
-        if (ga.dO)
-            load_tile(ga.dO + ((size_t)(t0 + c * GC) * a.H + h) * DV + col, vstep, gq,
-                      min(GC, t1 - t0 - c * GC), on);
-        else
+        for (int k = 0; k < KT; ++k) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) on[i] = from_f32<T>(0.f);
-    };
-    if (nch > 0) load_o(nch - 1);
+            for (int r = 0; r < 4; ++r)
+                dS[k][r] = ga.dS_T ? ga.dS_T[sbase + (size_t)(16 * k + r) * DV] : 0.f;
+            m = max_abs4(m, dS[k]);
+        }
+        // the first chunk is the only one that may be ragged
+        tile_offsets(vstep, vcol, gq, nch > 0 ? min(GC, t1 - t0 - (nch - 1) * GC) : GC, off);
+        if (nch > 0 && ga.dO) load_tile(vrow(ga.dO, nch - 1), off, on);
+        m = column_max(m);
+        float mv = m;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mv = fmaxf(mv, fabsf(Raw1<T>::f32(on[i])));
+        mv = column_max(mv);
+        if (mv > 0.f && mv < INFINITY) sU.renew(mv);
+        sS = sU;
+        if (m > 0.f && m < INFINITY) sS.renew(m * sS.s);
+#pragma unroll
+        for (int k = 0; k < KT; ++k) dS[k] = scaled(dS[k], sS.s);
+    }
     __syncthreads();
     for (int i = 0; i < nch; ++i) {
         const int c = nch - 1 - i;
@@ -114,154 +128,241 @@ __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_reverse_kernel(const Gra
         const char* tri = buf + Sh::O_REC + REC_HEAD;  // W^T hi, lo, A^T hi, lo
         const int len = min(GC, t1 - t0 - c * GC);
         auto factor = [&](int f, int b, float* x) { unpack4(ld4(fac + f * GC + 16 * b + 4 * gq), x); };
-        floatx4 G[4];
+        floatx4 V[4];  // dO
 #pragma unroll
         for (int b = 0; b < 4; ++b)
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                G[b][r] = 16 * b + 4 * gq + r < len ? to_f32(on[4 * b + r]) : 0.f;
-        if (c > 0) load_o(c - 1);
-        const size_t kept = (size_t)(g0 + c) * a.H + h;
-        float* kscale = ga.keep.scale + kept * KEEP_COUNT * (DV / 16) + col / 16;
-        keep_tile<Sh::P, DV, Sh::KT>(ga.keep.dS + kept * DK * DVP * Sh::P, kscale + KEEP_DS * (DV / 16),
-                                     dS, col, gq);
-
-        // K dS and A^T dO
-        float m = 0.f, sc, s_inv, g_inv;
+            for (int r = 0; r < 4; ++r) V[b][r] = Raw1<T>::f32(on[4 * b + r]);
+        float m = 0.f;
 #pragma unroll
-        for (int k = 0; k < Sh::KT; ++k) m = max_abs4(m, dS[k]);
-        pow2_scale(column_max(m), sc, s_inv);
-        Split sp[Sh::KSTEPS];
+        for (int k = 0; k < KT; ++k) m = max_abs4(m, dS[k]);
+        m = column_max(m);
+        if (__any(too_large(4.f * m) || (m < 16.f && m > 0.f))) {
+            const float f = too_large(4.f * m) || (m < 16.f && m > 0.f) ? sS.renew(m) : 1.f;
 #pragma unroll
-        for (int s = 0; s < Sh::KSTEPS; ++s)
-            sp[s] = split(dS[2 * s], Sh::KT > 1 ? dS[2 * s + 1] : zero4(), sc);
-        m = 0.f;
-#pragma unroll
-        for (int b = 0; b < 4; ++b) m = max_abs4(m, G[b]);
-        pow2_scale(column_max(m), sc, g_inv);
-        const Split gs[2] = {split(G[0], G[1], sc), split(G[2], G[3], sc)};  // bf16: lo = 0
-        floatx4 D[4], bd[4];
-        m = 0.f;
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            floatx4 x = zero4(), y = zero4();
-#pragma unroll
-            for (int s = 0; s < Sh::KSTEPS; ++s) {
-                const half8 kf = frag_ld(buf + Sh::O_K, b * Sh::KSTEPS + s, lane);
-                x = mma(kf, sp[s].hi, x);
-                x = mma(kf, sp[s].lo, x);
-                if (Sh::P == 2)
-                    x = mma(frag_ld(buf + Sh::O_K + Sh::RB, b * Sh::KSTEPS + s, lane), sp[s].hi, x);
-            }
-#pragma unroll
-            for (int s = b / 2; s < 2; ++s) {
-                const half8 af = frag_ld(tri, 2 * TRI + tri_frag_t(b, s), lane);
-                y = mma(af, gs[s].hi, y);
-                if (Sh::P == 2) y = mma(af, gs[s].lo, y);
-                y = mma(frag_ld(tri, 3 * TRI + tri_frag_t(b, s), lane), gs[s].hi, y);
-            }
-            float w[4], ar[4], be[4];
-            factor(F_W, b, w);
-            factor(F_ATR, b, ar);
-            factor(F_BE, b, be);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                D[b][r] = fmaf(w[r], x[r] * s_inv, ar[r] * (y[r] * g_inv));
-                bd[b][r] = be[r] * D[b][r];
-            }
-            m = max_abs4(m, bd[b]);
+            for (int k = 0; k < KT; ++k) dS[k] = scaled(dS[k], f);
         }
-        // Y = D - W^T (beta D)
-        float d_inv;
-        pow2_scale(column_max(m), sc, d_inv);
-        const Split ds[2] = {split(bd[0], bd[1], sc), split(bd[2], bd[3], sc)};
-        floatx4 z1[4], z2[4];
-        float m1 = 0.f, m2 = 0.f;
-        T* vp = ga.dv + ((size_t)(t0 + c * GC) * a.H + h) * DV + col;
+        Split sp[KS], s1[2], s2[2];
+        floatx4 y[4];
+        T out[16];
+        half8 kc[KT][2];
+        float mu;
+        for (int tries = 0;; ++tries) {  // as in gdr_walk
+            half8 kf[KS][4], ah[TRI], al[TRI];
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            floatx4 y = zero4();
+            for (int s = 0; s < KS; ++s)
 #pragma unroll
-            for (int s = b / 2; s < 2; ++s) {
-                const half8 wh = frag_ld(tri, tri_frag_t(b, s), lane);
-                y = mma(wh, ds[s].hi, y);
-                y = mma(wh, ds[s].lo, y);
-                y = mma(frag_ld(tri, TRI + tri_frag_t(b, s), lane), ds[s].hi, y);
+                for (int b = 0; b < 4; ++b) kf[s][b] = frag_rows<KS>(buf + Sh::O_K, lo, b, s);
+#pragma unroll
+            for (int j = 0; j < TRI; ++j) {
+                ah[j] = frag_ld(tri, 2 * TRI + j, lane);
+                al[j] = frag_ld(tri, 3 * TRI + j, lane);
             }
-            float wr[4], be[4], g1[4], g2[4];
-            factor(F_WTR, b, wr);
-            factor(F_BE, b, be);
-            factor(F_G1, b, g1);
-            factor(F_GQ, b, g2);
+            request_fence();
+            floatx4 G[4];
+            float mg = 0.f;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int t = 16 * b + 4 * gq + r;
-                D[b][r] = fmaf(-wr[r], y[r] * d_inv, D[b][r]);
-                const float dv = be[r] * D[b][r];
-                if (t < len) vp[(size_t)t * vstep] = from_f32<T>(dv);
-                z1[b][r] = g1[r] * dv;
-                z2[b][r] = g2[r] * G[b][r];
+            for (int b = 0; b < 4; ++b) {
+                G[b] = scaled(V[b], sU.s);
+                mg = max_abs4(mg, G[b]);
             }
-            m1 = max_abs4(m1, z1[b]);
-            m2 = max_abs4(m2, z2[b]);
-        }
-        keep_tile<Sh::P, DV, 4>(ga.keep.Y + kept * GC * DVP * Sh::P, kscale + KEEP_Y * (DV / 16), D, col,
-                                gq);
-        // dS <- 2^l_C dS + (2^l Q)^T dO - (2^l K)^T dV
-        float inv1, inv2, sc2;
-        pow2_scale(column_max(m1), sc, inv1);
-        pow2_scale(column_max(m2), sc2, inv2);
-        const Split s1[2] = {split(z1[0], z1[1], sc), split(z1[2], z1[3], sc)};
-        const Split s2[2] = {split(z2[0], z2[1], sc2), split(z2[2], z2[3], sc2)};
-        const float gc = fac[REC_FACTORS];
-#pragma unroll
-        for (int k = 0; k < Sh::KT; ++k) {
-            floatx4 x = zero4(), y = zero4();
+            Split gs[2];  // of a bf16 dO the low halves are 0
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
-                const half8 kf = frag_ld(buf + Sh::O_KT, 2 * k + s, lane);
-                x = mma(kf, s1[s].hi, x);
-                x = mma(kf, s1[s].lo, x);
-                const half8 qf = frag_ld(buf + Sh::O_QT, 2 * k + s, lane);
-                y = mma(qf, s2[s].hi, y);
-                y = mma(qf, s2[s].lo, y);
-                if (Sh::P == 2) {
-                    x = mma(frag_ld(buf + Sh::O_KT + Sh::CB, 2 * k + s, lane), s1[s].hi, x);
-                    y = mma(frag_ld(buf + Sh::O_QT + Sh::CB, 2 * k + s, lane), s2[s].hi, y);
-                }
+                if (P == 2)
+                    gs[s] = split(G[2 * s], G[2 * s + 1]);
+                else
+                    gs[s].hi = to_half(G[2 * s], G[2 * s + 1]);
             }
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                dS[k][r] = fmaf(gc, dS[k][r], fmaf(y[r], inv2, -(x[r] * inv1)));
+            for (int s = 0; s < KS; ++s) sp[s] = split(dS[2 * s], KT > 1 ? dS[2 * s + 1] : zero4());
+            request_fence();
+            // K dS and A^T dO
+            floatx4 x[4], d[4], D[4];
+            float w[4][4], ar[4][4], be[4][4];
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                factor(F_W, b, w[b]);
+                factor(F_ATR, b, ar[b]);
+                factor(F_BE, b, be[b]);
+                x[b] = zero4();
+                d[b] = zero4();
+            }
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+#pragma unroll
+                for (int b = 0; b < 4; ++b) x[b] = mma(kf[s][b], sp[s].hi, x[b]);
+#pragma unroll
+                for (int b = 0; b < 4; ++b) x[b] = mma(kf[s][b], sp[s].lo, x[b]);
+                if (P == 2)
+#pragma unroll
+                    for (int b = 0; b < 4; ++b)
+                        x[b] = mma(frag_rows<KS>(buf + Sh::O_K + Sh::RB, lo, b, s), sp[s].hi, x[b]);
+            }
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+#pragma unroll
+                for (int b = 0; b < 2 * s + 2; ++b) d[b] = mma(ah[tri_frag_t(b, s)], gs[s].hi, d[b]);
+#pragma unroll
+                for (int b = 0; b < 2 * s + 2; ++b) d[b] = mma(al[tri_frag_t(b, s)], gs[s].hi, d[b]);
+                if (P == 2)
+#pragma unroll
+                    for (int b = 0; b < 2 * s + 2; ++b) d[b] = mma(ah[tri_frag_t(b, s)], gs[s].lo, d[b]);
+            }
+            request_fence();
+            half8 wh[TRI], wl[TRI];
+#pragma unroll
+            for (int j = 0; j < TRI; ++j) {
+                wh[j] = frag_ld(tri, j, lane);
+                wl[j] = frag_ld(tri, TRI + j, lane);
+            }
+            float wr[4][4], g1[4][4], g2[4][4];
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                factor(F_WTR, b, wr[b]);
+                factor(F_G1, b, g1[b]);
+                factor(F_GQ, b, g2[b]);
+            }
+            request_fence();
+            const float xs = sU.s * sS.i, zs = sS.s * sU.i;
+            float mb = 0.f;
+            floatx4 bd[4];
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    D[b][r] = fmaf(w[b][r], x[b][r] * xs, ar[b][r] * d[b][r]);
+                    bd[b][r] = be[b][r] * D[b][r];
+                }
+                mb = max_abs4(mb, bd[b]);
+            }
+            const Split ds[2] = {split(bd[0], bd[1]), split(bd[2], bd[3])};
+            request_fence();
+            // Y = D - W^T (beta D)
+#pragma unroll
+            for (int k = 0; k < KT; ++k)
+#pragma unroll
+                for (int s = 0; s < 2; ++s) kc[k][s] = frag_cols<KS>(buf + Sh::O_K, lo, k, s);
+#pragma unroll
+            for (int b = 0; b < 4; ++b) d[b] = zero4();
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+#pragma unroll
+                for (int b = 0; b < 2 * s + 2; ++b) d[b] = mma(wh[tri_frag_t(b, s)], ds[s].hi, d[b]);
+#pragma unroll
+                for (int b = 0; b < 2 * s + 2; ++b) d[b] = mma(wh[tri_frag_t(b, s)], ds[s].lo, d[b]);
+#pragma unroll
+                for (int b = 0; b < 2 * s + 2; ++b) d[b] = mma(wl[tri_frag_t(b, s)], ds[s].hi, d[b]);
+            }
+            request_fence();
+            floatx4 z1[4], z2[4];
+            float mz = 0.f;
+            mu = mg;
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    y[b][r] = fmaf(-wr[b][r], d[b][r], D[b][r]);
+                    const float dv = be[b][r] * y[b][r];
+                    out[4 * b + r] = from_f32<T>(dv * sU.i);
+                    z1[b][r] = (-g1[b][r] * zs) * dv;
+                    z2[b][r] = (g2[b][r] * zs) * G[b][r];
+                }
+                mu = max_abs4(mu, y[b]);
+                mz = max_abs4(max_abs4(mz, z1[b]), z2[b]);
+            }
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                s1[s] = split(z1[2 * s], z1[2 * s + 1]);
+                s2[s] = split(z2[2 * s], z2[2 * s + 1]);
+            }
+            if (!__any(too_large(mb) || too_large(mu) || too_large(mz)) || tries == 8) break;
+            mg = column_max(mg);
+            mb = column_max(mb);
+            mu = column_max(mu);
+            mz = column_max(mz);
+            float f = 1.f;
+            if (too_large(mg))
+                sU.renew(mg);
+            else if (too_large(mb))
+                sU.renew(mb);
+            else if (too_large(mu))
+                sU.renew(mu);
+            else if (too_large(mz))
+                f = sS.renew(mz);
+#pragma unroll
+            for (int k = 0; k < KT; ++k) dS[k] = scaled(dS[k], f);
         }
+        half8 qc[KT][2];
+#pragma unroll
+        for (int k = 0; k < KT; ++k)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) qc[k][s] = frag_cols<KS>(buf + Sh::O_Q, lo, k, s);
+        request_fence();
+        store_tile(vrow(ga.dv, c), off, gq, len, out);
+        if (i == 0) tile_offsets(vstep, vcol, gq, GC, off);
+        if (c > 0 && ga.dO) load_tile(vrow(ga.dO, c - 1), off, on);
+        {
+            const size_t kept = (size_t)(g0 + c) * a.H + h;
+            _Float16* ks = ga.keep.dS + kept * keep_state<T, DK>(DV) + (size_t)(ctile * KS * 64 + lane) * 8;
+            _Float16* ky = ga.keep.Y + kept * keep_rows<T>(DV) + (size_t)(ctile * 2 * 64 + lane) * 8;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                st8(ks + s * 512, sp[s].hi);
+                if (P == 2) st8(ks + (DV / 16 * KS + s) * 512, sp[s].lo);
+            }
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const Split x = split(y[2 * s], y[2 * s + 1]);
+                st8(ky + s * 512, x.hi);
+                if (P == 2) st8(ky + (DV / 16 * 2 + s) * 512, x.lo);
+            }
+            float* sc = ga.keep.scale + kept * KEEP_COUNT * DV + col;
+            if (gq == 0) {
+                sc[KEEP_DS * DV] = sS.i;
+                sc[KEEP_Y * DV] = sU.i;
+            }
+        }
+        // dS <- 2^l_C dS + (2^l Q)^T dO - (2^l K)^T dV
+        const float gc = fac[REC_FACTORS];
+#pragma unroll
+        for (int k = 0; k < KT; ++k) dS[k] = scaled(dS[k], gc);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+#pragma unroll
+            for (int k = 0; k < KT; ++k) dS[k] = mma(kc[k][s], s1[s].hi, dS[k]);
+#pragma unroll
+            for (int k = 0; k < KT; ++k) dS[k] = mma(kc[k][s], s1[s].lo, dS[k]);
+#pragma unroll
+            for (int k = 0; k < KT; ++k) dS[k] = mma(qc[k][s], s2[s].hi, dS[k]);
+#pragma unroll
+            for (int k = 0; k < KT; ++k) dS[k] = mma(qc[k][s], s2[s].lo, dS[k]);
+            if (P == 2)
+#pragma unroll
+                for (int k = 0; k < KT; ++k) {
+                    dS[k] = mma(frag_cols<KS>(buf + Sh::O_K + Sh::RB, lo, k, s), s1[s].hi, dS[k]);
+                    dS[k] = mma(frag_cols<KS>(buf + Sh::O_Q + Sh::RB, lo, k, s), s2[s].hi, dS[k]);
+                }
+        }
+        mu = column_max(mu);
+        if (mu < 4.f && mu > 0.f) sU.renew(mu);
         if (Sh::NBUF == 1) __syncthreads();
         __syncthreads();
     }
     if (ga.dS0)
 #pragma unroll
-        for (int k = 0; k < Sh::KT; ++k)
+        for (int k = 0; k < KT; ++k)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) ga.dS0[sbase + (size_t)(16 * k + r) * DV] = dS[k][r];
+            for (int r = 0; r < 4; ++r) ga.dS0[sbase + (size_t)(16 * k + r) * DV] = dS[k][r] * sS.i;
 }
 
 // ------------------------------------------------------------------------------------------
-// gdr_grad: a workgroup per (chunk, key head), wave w has tokens 16w .. 16w+15; the value heads of the
-// key head one after another, dQ and dK summed in registers in that order.
+// gdr_grad: a workgroup of eight waves per (chunk, key head); wave (w, half) has tokens 16w .. 16w+15
+// and, of the products with the state, half of the key channels; the value heads of the key head one
+// after another, dQ and dK summed in registers in that order. E and Y, then S and dS come through LDS,
+// from where the transposing read gives either side's fragments; the scales of the value columns, over
+// which the products contract, are folded into the A side (each over the largest).
 // ------------------------------------------------------------------------------------------
-constexpr int CP = 68;  // floats of a row of the 64 x 64 matrices in LDS
-
-__device__ __forceinline__ float pow2_inverse(float x)  // of a power of two in [2^-126, 2^126]
-{
-    return __uint_as_float(0x7f000000u - __float_as_uint(x));
-}
-
-// A fragment's slots of the two 16-value blocks times f0 and f1 (powers of two, at most 1).
-__device__ __forceinline__ half8 fold(half8 x, float f0, float f1)
-{
-    const _Float16 a = (_Float16)f0, b = (_Float16)f1;
-    return x * half8{a, a, a, a, b, b, b, b};
-}
-
 template <int P, int N>
 struct Operand {
     half8 hi[N], lo[P == 2 ? N : 1];
@@ -279,47 +380,100 @@ __device__ __forceinline__ floatx4 mma_parts(half8 ah, half8 al, half8 bh, half8
     return acc;
 }
 
-template <class T, int DK, int DV>
-__global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) void gdr_grad_kernel(const GradArgs<T> ga)
+// The products over the value columns and the two scales that each has to carry.
+enum { FOLD_E, FOLD_YE, FOLD_S, FOLD_YS, FOLD_ED, FOLD_COUNT };
+
+__device__ __forceinline__ int col_place(int n)  // of column n among those of a fragment's lanes
 {
-    using Sh = ChunkLds<T, DK, false, true, false, true, -1>;
-    using Fr = Frag<T, DK>;
-    using V = typename Fr::V;
-    constexpr int P = Sh::P, REC = gdr_rec_bytes<T, true>();
-    constexpr int DVP = DV < 32 ? 32 : DV, VS = DVP / 32, NB = DV / 16;
+    return (n & ~31) + ((n & 15) >> 2) * 8 + (n & 3) + ((n >> 4) & 1) * 4;
+}
+
+// Sum over the lanes before this one in its row of 16 (never a difference: what stands at a lane may
+// be far larger than what stands before it).
+__device__ __forceinline__ float before16(float x)
+{
+    x = dpp_add<0x111, 0xf>(x);  // row_shr 1, 2, 4, 8: inclusive
+    x = dpp_add<0x112, 0xf>(x);
+    x = dpp_add<0x114, 0xf>(x);
+    x = dpp_add<0x118, 0xf>(x);
+    return __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), 0x111, 0xf,
+                                                                 0xf, false));
+}
+
+template <class T, int DK, int DV>
+struct GradLds {
+    using Sh = ChunkLds<T, DK, true, -1>;
+    static constexpr int P = Sh::P;
+    static constexpr int ROWS = (int)keep_rows<T>(DV) * 2;        // bytes of E or Y
+    static constexpr int STATE = (int)keep_state<T, DK>(DV) * 2;  // of S or dS
+    static constexpr bool BOTH = P == 1;                          // S and dS at once
+    static constexpr int R = 2 * ROWS > (BOTH ? 2 : 1) * STATE ? 2 * ROWS : (BOTH ? 2 : 1) * STATE;
+};
+
+constexpr int CP = 68;  // floats of a row of the 64 x 64 matrix in LDS
+
+template <class T, int DK, int DV>
+__global__ __launch_bounds__(512) void gdr_grad_kernel(const GradArgs<T> ga)
+{
+    using Ls = GradLds<T, DK, DV>;
+    using Sh = typename Ls::Sh;
+    constexpr int P = Sh::P, KS = Sh::KSTEPS, KT = Sh::KT, NT = 512;
+    constexpr int REC = gdr_rec_bytes<T, true>();
+    constexpr int VS = DV < 32 ? 1 : DV / 32, VT = DV / 16, KH = (KT + 1) / 2;
+    constexpr int DVP = VS * 32;
     const ChunkArgs<T>& a = ga.c;
-    __shared__ __align__(16) char lds[Sh::BYTES];
-    __shared__ __align__(16) float sC[GC * CP];  // C on and below the diagonal, Z^T above it
-    __shared__ __align__(16) float sP[GC * CP];  // the pairs' share of the log-decay's gradient
+    __shared__ __align__(16) char lds[Sh::BYTES];     // K, Q
+    __shared__ __align__(16) char reg[Ls::R];         // E and Y, then S and dS
+    __shared__ __align__(16) float sC[GC * CP];       // C on and below the diagonal, Z^T above it
+    __shared__ __align__(16) _Float16 s_fold[FOLD_COUNT][DVP];
+    __shared__ float s_top[FOLD_COUNT], s_inv[KEEP_COUNT][DV];
     __shared__ double s_l[GC];
-    __shared__ float s_be[GC], s_ri[GC], s_reads[GC], s_writes[GC], s_dot[4];
+    __shared__ float s_be[GC], s_ri[GC], s_ks[GC], s_qs[GC], s_dot[8];
+    __shared__ float s_reads[2][GC], s_writes[2][GC], s_cross[4][GC], s_tot[GC];
     __shared__ float s_ic[GC], s_it[GC], s_iz[GC];  // inverse scales of the rows of C, C^T, Z + Z^T
     const int g = blockIdx.x / a.Hk, hk = blockIdx.x % a.Hk;
     int n, c0, c1;
     if (!gdr_locate(a.seq, g, n, c0, c1)) return;
-    const int len = c1 - c0, tid = threadIdx.x, w = tid >> 6, lane = tid & 63, gq = lane >> 4,
-              li = lane & 15, row = 16 * w + li;
+    const int len = c1 - c0, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, gq = lane >> 4,
+              li = lane & 15, w = wave & 3, half = wave >> 2, row = 16 * w + li;
+    const LaneOffsets lo(lane);
+    const int tr = lo.tr[0];
 
-    const T* kbase = a.k + ((size_t)c0 * a.Hk + hk) * DK;
-    const T* qbase = a.q + ((size_t)c0 * a.Hk + hk) * DK;
-    const size_t kstep = (size_t)a.Hk * DK;
+    if (DK == 16) {  // the upper half of the 32 contracted places stays 0
+        for (int i = tid; i < Sh::BYTES / 16; i += NT)
+            reinterpret_cast<uint4*>(lds)[i] = make_uint4(0, 0, 0, 0);
+        __syncthreads();
+    }
     const char* rec = a.rec + ((size_t)g * a.H + (size_t)hk * a.rep) * REC;
     {
-        Loader<T, DK, Sh, 256, 0> ld;
-        ld.load(kbase, qbase, kstep, tid, len, rec);
+        Loader<T, DK, Sh, NT, 0> ld;
+        const size_t at = ((size_t)c0 * a.Hk + hk) * DK;
+        ld.load(a.k + at, a.q + at, (unsigned)(a.Hk * DK * sizeof(T)), tid, len, rec);
         ld.store(lds, tid);
-    }
-    auto load_rows = [&](const T* base, int b, V* f) {
-        const int t = 16 * b + li;
-#pragma unroll
-        for (int s = 0; s < Fr::NS; ++s) {
-            f[s] = V{};
-            if (t < len) f[s] = Fr::ld(base + t * kstep + gq * (Fr::KF / 4) + s * Fr::KF);
+        const float* fac = reinterpret_cast<const float*>(rec);
+        if (tid < GC) {  // 0 for the tokens past the end, as the rows' scales
+            s_ks[tid] = fac[F_KS * GC + tid] > 0.f ? pow2_inverse(fac[F_KS * GC + tid]) : 0.f;
+            s_qs[tid] = fac[F_QS * GC + tid] > 0.f ? pow2_inverse(fac[F_QS * GC + tid]) : 0.f;
         }
-    };
-    floatx4 dq[Sh::KT], dk[Sh::KT];
+    }
+    floatx4 dq[KH], dk[KH];
 #pragma unroll
-    for (int k = 0; k < Sh::KT; ++k) dq[k] = dk[k] = zero4();
+    for (int k = 0; k < KH; ++k) dq[k] = dk[k] = zero4();
+
+    // fragments of E or Y: tokens 16b .. as rows, value columns 32s ..
+    auto rows_frag = [&](const char* x, int b, int s) {
+        const char* p = x + (b >> 1) * 1024 + (b & 1) * 8 + tr;
+        const half4 y = lds_read_tr(p + 2 * s * 2048);
+        const half4 z = VT > 1 ? lds_read_tr(p + (2 * s + 1) * 2048) : half4{0, 0, 0, 0};
+        return __builtin_shufflevector(y, z, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    // of S or dS: key channels 16k .. as rows, value columns 32s ..
+    auto state_frag = [&](const char* x, int k, int s) {
+        const char* p = x + (k >> 1) * 1024 + (k & 1) * 8 + tr;
+        const half4 y = lds_read_tr(p + 2 * s * KS * 1024);
+        const half4 z = VT > 1 ? lds_read_tr(p + (2 * s + 1) * KS * 1024) : half4{0, 0, 0, 0};
+        return __builtin_shufflevector(y, z, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
 
 #pragma unroll 1
     for (int hv = 0; hv < a.rep; ++hv) {
@@ -327,161 +481,230 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) void gdr_grad_kernel(c
         const size_t kept = (size_t)g * a.H + h;
         rec = a.rec + kept * REC;
         const float* fac = reinterpret_cast<const float*>(rec);
-        const float* ksc = ga.keep.scale + kept * KEEP_COUNT * NB;
-        const float gamma = fac[REC_FACTORS];
+        const uint4* gE = reinterpret_cast<const uint4*>(ga.keep.E + kept * keep_rows<T>(DV));
+        const uint4* gY = reinterpret_cast<const uint4*>(ga.keep.Y + kept * keep_rows<T>(DV));
+        const uint4* gS = reinterpret_cast<const uint4*>(ga.keep.S + kept * keep_state<T, DK>(DV));
+        const uint4* gD = reinterpret_cast<const uint4*>(ga.keep.dS + kept * keep_state<T, DK>(DV));
+        for (int i = tid; i < Ls::ROWS / 16; i += NT) {
+            reinterpret_cast<uint4*>(reg)[i] = gE[i];
+            reinterpret_cast<uint4*>(reg + Ls::ROWS)[i] = gY[i];
+        }
         if (tid < GC) {
             s_l[tid] = reinterpret_cast<const double*>(fac + F_L * GC)[tid];
             s_be[tid] = fac[F_BE * GC + tid];
         }
-        const _Float16* E = ga.keep.E + kept * GC * DVP * P;
-        const _Float16* Y = ga.keep.Y + kept * GC * DVP * P;
-        const _Float16* S = ga.keep.S + kept * DK * DVP * P;
-        const _Float16* dS = ga.keep.dS + kept * DK * DVP * P;
-        // this wave's rows of dO (scaled by row; the inverse scales to s_ri), and of E or Y
-        auto load_dO = [&]() {
-            Operand<P, VS> go;
+        for (int i = tid; i < KEEP_COUNT * DV; i += NT)
+            s_inv[i / DV][i % DV] = ga.keep.scale[kept * KEEP_COUNT * DV + i];
+        // this wave's rows of dO, scaled by row (the inverse scales to s_ri)
+        Operand<P, VS> go;
+        {
             float x[VS][8], m = 0.f;
-            const T* p = ga.dO + ((size_t)(c0 + row) * a.H + h) * DV + 4 * gq;
+            const T* p = ga.dO + ((size_t)(c0 + min(row, len - 1)) * a.H + h) * DV + 4 * gq;
 #pragma unroll
             for (int s = 0; s < VS; ++s)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    x[s][e] = 0.f;
-                    if (ga.dO && row < len && (DV >= 32 || e < 4))
-                        x[s][e] = to_f32(p[32 * s + (e & 3) + 16 * (e >> 2)]);
-                    m = fmaxf(m, fabsf(x[s][e]));
+                for (int u = 0; u < 2; ++u) {
+                    struct alignas(4 * sizeof(T)) V4 { T v[4]; };
+                    V4 y = {};
+                    if (ga.dO && (u == 0 || VT > 1)) y = *reinterpret_cast<const V4*>(p + 32 * s + 16 * u);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        x[s][4 * u + e] = row < len ? to_f32(y.v[e]) : 0.f;
+                        m = fmaxf(m, fabsf(x[s][4 * u + e]));
+                    }
                 }
             float sc, inv;
-            pow2_scale(column_max(m), sc, inv);
-#pragma unroll
-            for (int s = 0; s < VS; ++s)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float z = x[s][e] * sc;
-                    go.hi[s][e] = (_Float16)z;
-                    if (P == 2) go.lo[s][e] = (_Float16)(z - (float)go.hi[s][e]);
-                }
-            if (gq == 0) s_ri[row] = inv;
-            return go;
-        };
-        auto kept_row = [&](const _Float16* x, int r, int s) {
-            return *reinterpret_cast<const half8*>(x + r * DVP + 32 * s + 8 * gq);
-        };
-        auto load_kept = [&](const _Float16* x) {
-            Operand<P, VS> y;
+            pow2_scale<0>(column_max(m), sc, inv);
 #pragma unroll
             for (int s = 0; s < VS; ++s) {
-                y.hi[s] = kept_row(x, row, s);
-                if (P == 2) y.lo[s] = kept_row(x + GC * DVP, row, s);
-            }
-            return y;
-        };
-        // the tiles' scales, and of the products over the value columns: the largest, and the others
-        // over it (folded into the A side)
-        float iS[2 * VS], iE[2 * VS], iD[2 * VS], iY[2 * VS];
 #pragma unroll
-        for (int j = 0; j < 2 * VS; ++j) {
-            iS[j] = j < NB ? ksc[KEEP_S * NB + j] : 0.f;
-            iE[j] = j < NB ? ksc[KEEP_E * NB + j] : 0.f;
-            iD[j] = j < NB ? ksc[KEEP_DS * NB + j] : 0.f;
-            iY[j] = j < NB ? ksc[KEEP_Y * NB + j] : 0.f;
+                for (int e = 0; e < 8; ++e) x[s][e] *= sc;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) go.hi[s][e] = (_Float16)x[s][e];
+                if (P == 2) {
+                    go.hi[s] = fixed_half(go.hi[s]);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) go.lo[s][e] = (_Float16)(x[s][e] - (float)go.hi[s][e]);
+                }
+            }
+            if (half == 0 && gq == 0) s_ri[row] = inv;
         }
-        auto operand = [&](const Operand<P, VS>& x, const float* f1, const float* f2, float& top) {
-            Operand<P, VS> y;
-            float f[2 * VS];
-            top = 0x1p-126f;
+        __syncthreads();
+        if (wave < FOLD_COUNT) {  // a wave per product: its columns' scales over the largest
+            constexpr int first[FOLD_COUNT] = {KEEP_E, KEEP_Y, KEEP_S, KEEP_Y, KEEP_E};
+            constexpr int second[FOLD_COUNT] = {-1, KEEP_E, -1, KEEP_S, KEEP_DS};
+            int f1 = 0, f2 = 0;
 #pragma unroll
-            for (int j = 0; j < 2 * VS; ++j) {
-                f[j] = f2 ? f1[j] * f2[j] : f1[j];
-                top = fmaxf(top, f[j]);
+            for (int i = 0; i < FOLD_COUNT; ++i)
+                if (wave == i) {
+                    f1 = first[i];
+                    f2 = second[i];
+                }
+            float x[2];
+            float top = 0x1p-120f;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int i = lane + 64 * j;
+                x[j] = i < DV ? s_inv[f1][i] * (f2 < 0 ? 1.f : s_inv[f2][i]) : 0.f;
+                top = fmaxf(top, x[j]);
             }
+            top = fminf(wave_max(top), 0x1p120f);
             const float r = pow2_inverse(top);
 #pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int i = lane + 64 * j;
+                if (i < DVP) s_fold[wave][col_place(i)] = (_Float16)(x[j] * r);
+            }
+            if (lane == 0) s_top[wave] = top;
+        }
+        // S and dS on their way while the 64 x 64 products run
+        constexpr int SP = (Ls::STATE / 16 + NT - 1) / NT;
+        uint4 bS[SP], bD[SP];
+#pragma unroll
+        for (int j = 0; j < SP; ++j) {
+            const int i = min(tid + NT * j, Ls::STATE / 16 - 1);
+            bS[j] = gS[i];
+            bD[j] = gD[i];
+        }
+        __syncthreads();
+        auto folded = [&](const Operand<P, VS>& x, int f) {
+            Operand<P, VS> y;
+#pragma unroll
             for (int s = 0; s < VS; ++s) {
-                y.hi[s] = fold(x.hi[s], f[2 * s] * r, f[2 * s + 1] * r);
-                if (P == 2) y.lo[s] = fold(x.lo[s], f[2 * s] * r, f[2 * s + 1] * r);
+                const half8 m = *reinterpret_cast<const half8*>(&s_fold[f][32 * s + 8 * gq]);
+                y.hi[s] = x.hi[s] * m;
+                if (P == 2) y.lo[s] = x.lo[s] * m;
             }
             return y;
         };
-        // dbeta = rowsum(Y E); the A sides of the 64 x 64 products
-        float top1, top2;
-        Operand<P, VS> goE, yeE;
+        // rows of E and Y; dbeta = rowsum(Y E)
+        Operand<P, VS> ee, ye;
         {
-            const Operand<P, VS> ye = load_kept(Y), ee = load_kept(E);
             float x = 0.f;
 #pragma unroll
             for (int s = 0; s < VS; ++s) {
-                float y0 = 0.f, y1 = 0.f;
+                ee.hi[s] = rows_frag(reg, w, s);
+                ye.hi[s] = rows_frag(reg + Ls::ROWS, w, s);
+                if (P == 2) {
+                    ee.lo[s] = rows_frag(reg + Ls::ROWS / 2, w, s);
+                    ye.lo[s] = rows_frag(reg + Ls::ROWS + Ls::ROWS / 2, w, s);
+                }
+                if (half == 0)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float p = (float)ye.hi[s][e], q = (float)ee.hi[s][e];
-                    if (P == 2) {
-                        p += (float)ye.lo[s][e];
-                        q += (float)ee.lo[s][e];
+                    for (int e = 0; e < 8; ++e) {
+                        const int i = 32 * s + 4 * gq + (e & 3) + 16 * (e >> 2);
+                        if (i >= DV) continue;
+                        float y = (float)ye.hi[s][e], z = (float)ee.hi[s][e];
+                        if (P == 2) {
+                            y += (float)ye.lo[s][e];
+                            z += (float)ee.lo[s][e];
+                        }
+                        x += (y * s_inv[KEEP_Y][i]) * (z * s_inv[KEEP_E][i]);
                     }
-                    (e < 4 ? y0 : y1) += p * q;
-                }
-                x += y0 * iY[2 * s] * iE[2 * s] + y1 * iY[2 * s + 1] * iE[2 * s + 1];
             }
-            x = column_sum(x);
-            if (gq == 0 && row < len) ga.dbeta[(size_t)(c0 + row) * a.H + h] = from_f32<T>(x);
-            goE = operand(load_dO(), iE, nullptr, top1);
-            yeE = operand(ye, iY, iE, top2);
+            if (half == 0) {
+                x = column_sum(x);
+                if (gq == 0 && row < len) ga.dbeta[(size_t)(c0 + row) * a.H + h] = from_f32<T>(x);
+            }
         }
-        __syncthreads();  // s_l, s_be, s_ri (and the K, Q fragments)
-
-        // C, Z and the pairs' share of the log-decay's gradient
+        // C, Z and the pairs' share of the log-decay's gradient: column blocks 2 half, 2 half + 1
         {
-            V fk[Fr::NS], fq[Fr::NS];
-            load_rows(kbase, w, fk);
-            load_rows(qbase, w, fq);
-            double lr[4];
-            float br[4], ri[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                lr[r] = s_l[16 * w + 4 * gq + r];
-                br[r] = s_be[16 * w + 4 * gq + r];
-                ri[r] = s_ri[16 * w + 4 * gq + r];
-            }
+            const Operand<P, VS> goE = folded(go, FOLD_E), yeE = folded(ye, FOLD_YE);
+            const float top1 = s_top[FOLD_E], top2 = s_top[FOLD_YE];
+            float carry[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
-            for (int c = 0; c < 4; ++c) {
-                const int s = 16 * c + li;
-                if (c > w) {
+            for (int c = 2 * half; c < 2 * half + 2; ++c) {
+                float cs = 0.f;
+                if (c <= w) {
+                    floatx4 kk = zero4(), qk = zero4(), d1 = zero4(), d2 = zero4();
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) sP[(16 * w + 4 * gq + r) * CP + s] = 0.f;
-                    continue;
-                }
-                V fc[Fr::NS];
-                load_rows(kbase, c, fc);
-                floatx4 kk = zero4(), qk = zero4(), d1 = zero4(), d2 = zero4();
+                    for (int i = 0; i < KS; ++i) {
+                        // rows of either block: c and w are not known at compile time
+                        auto frag = [&](int o, int b) {
+                            const int r = (i + KS * b) & 3;
+                            return *reinterpret_cast<const half8*>(
+                                lds + o + (b * KS + i) * 1024 + gq * 256 + ((li + r) & 15) * 16);
+                        };
+                        const half8 kh = frag(Sh::O_K, c), kw = frag(Sh::O_K, w), qw = frag(Sh::O_Q, w);
+                        half8 kl = kh, kwl = kw, qwl = qw;
+                        if (P == 2) {
+                            kl = frag(Sh::O_K + Sh::RB, c);
+                            kwl = frag(Sh::O_K + Sh::RB, w);
+                            qwl = frag(Sh::O_Q + Sh::RB, w);
+                        }
+                        kk = mma_parts<P>(kw, kwl, kh, kl, kk);
+                        qk = mma_parts<P>(qw, qwl, kh, kl, qk);
+                    }
 #pragma unroll
-                for (int i = 0; i < Fr::NS; ++i) {
-                    kk = Fr::mma(kk, fk[i], fc[i]);
-                    qk = Fr::mma(qk, fq[i], fc[i]);
-                }
+                    for (int i = 0; i < VS; ++i) {
+                        const half8 eh = rows_frag(reg, c, i);
+                        half8 el = eh;
+                        if (P == 2) el = rows_frag(reg + Ls::ROWS / 2, c, i);
+                        d1 = mma_parts<P>(goE.hi[i], goE.lo[P == 2 ? i : 0], eh, el, d1);
+                        d2 = mma_parts<P>(yeE.hi[i], yeE.lo[P == 2 ? i : 0], eh, el, d2);
+                    }
+                    const int s = 16 * c + li;
+                    const double ls = s_l[s];
+                    const float bs = s_be[s], ks = s_ks[s];
 #pragma unroll
-                for (int i = 0; i < VS; ++i) {
-                    const half8 eh = kept_row(E, s, i);
-                    half8 el = eh;
-                    if (P == 2) el = kept_row(E + GC * DVP, s, i);
-                    d1 = mma_parts<P>(goE.hi[i], goE.lo[P == 2 ? i : 0], eh, el, d1);
-                    d2 = mma_parts<P>(yeE.hi[i], yeE.lo[P == 2 ? i : 0], eh, el, d2);
+                    for (int r = 0; r < 4; ++r) {
+                        const int t = 16 * w + 4 * gq + r;
+                        const float rho =
+                            t >= s ? bs * __builtin_amdgcn_exp2f((float)(s_l[t] - ls)) : 0.f;
+                        const float cc = t >= s ? a.scale * rho * (d1[r] * top1 * s_ri[t]) : 0.f;
+                        const float zz = t > s ? -s_be[t] * rho * (d2[r] * top2) : 0.f;
+                        if (t >= s) sC[t * CP + s] = cc;
+                        if (t > s) sC[s * CP + t] = zz;
+                        const float p = (cc * (qk[r] * s_qs[t]) + zz * (kk[r] * s_ks[t])) * ks;
+                        // what stands before place s in the row, down the column from the diagonal
+                        const float before = carry[r] + before16(p);
+                        cs += t >= s ? before : 0.f;
+                        carry[r] += row16_sum(p);
+                    }
                 }
-                const double ls = s_l[s];
-                const float bs = s_be[s];
+                cs = column_sum(cs);
+                if (gq == 0) s_cross[w][16 * c + li] = cs;
+            }
+            if (half == 0 && li == 0)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int t = 16 * w + 4 * gq + r;
-                    const float rho = t >= s ? bs * __builtin_amdgcn_exp2f((float)(lr[r] - ls)) : 0.f;
-                    const float cc = t >= s ? a.scale * rho * (d1[r] * top1 * ri[r]) : 0.f;
-                    const float zz = t > s ? -br[r] * rho * (d2[r] * top2) : 0.f;
-                    if (t >= s) sC[t * CP + s] = cc;
-                    if (t > s) sC[s * CP + t] = zz;
-                    sP[t * CP + s] = cc * qk[r] + zz * kk[r];
+                for (int r = 0; r < 4; ++r) s_tot[16 * w + 4 * gq + r] = carry[r];
+        }
+        // <S, dS>, then both to LDS
+        float dot = 0.f;
+#pragma unroll
+        for (int j = 0; j < SP; ++j) {
+            const int i = tid + NT * j;
+            if (i >= Ls::STATE / 16 / P) continue;  // P = 2: with the low halves, read here
+            const half8 sh = __builtin_bit_cast(half8, bS[j]), dh = __builtin_bit_cast(half8, bD[j]);
+            float x = 0.f;
+            half8 sl = sh, dl = dh;
+            if (P == 2) {
+                sl = __builtin_bit_cast(half8, gS[i + Ls::STATE / 32]);
+                dl = __builtin_bit_cast(half8, gD[i + Ls::STATE / 32]);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float y = (float)sh[e], z = (float)dh[e];
+                if (P == 2) {
+                    y += (float)sl[e];
+                    z += (float)dl[e];
                 }
+                x += y * z;
+            }
+            const int col = i / (64 * KS) * 16 + (i & 15);
+            dot += (x * s_inv[KEEP_S][col]) * s_inv[KEEP_DS][col];
+        }
+        dot = wave_sum(dot);
+        if (lane == 0) s_dot[wave] = dot;
+        __syncthreads();  // E and Y are read, C and Z written
+#pragma unroll
+        for (int j = 0; j < SP; ++j) {
+            const int i = tid + NT * j;
+            if (i < Ls::STATE / 16) {
+                reinterpret_cast<uint4*>(reg)[i] = bS[j];
+                if (Ls::BOTH) reinterpret_cast<uint4*>(reg + Ls::STATE)[i] = bD[j];
             }
         }
-        __syncthreads();
         // C's rows, its columns and the rows of Z + Z^T as operands, over the scales of the K or Q rows
         // that they meet
         Operand<P, 2> opC, opT, opZ;
@@ -492,155 +715,174 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) void gdr_grad_kernel(c
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const int j = 32 * s + 4 * gq + (e & 3) + 16 * (e >> 2);
-                    const float ki = pow2_inverse(fac[F_KS * GC + j]), qi = pow2_inverse(fac[F_QS * GC + j]);
                     const float y = sC[row * CP + j], z = sC[j * CP + row];
-                    x[0][s][e] = j <= row ? y * ki : 0.f;
-                    x[1][s][e] = j >= row ? z * qi : 0.f;
-                    x[2][s][e] = j < row ? z * ki : j > row ? y * ki : 0.f;
+                    x[0][s][e] = j <= row ? y * s_ks[j] : 0.f;
+                    x[1][s][e] = j >= row ? z * s_qs[j] : 0.f;
+                    x[2][s][e] = (j < row ? z : j > row ? y : 0.f) * s_ks[j];
 #pragma unroll
                     for (int i = 0; i < 3; ++i) m[i] = fmaxf(m[i], fabsf(x[i][s][e]));
                 }
-            float sc[3], inv[3];
+            auto convert = [&](float (*y)[8], float m, Operand<P, 2>& op, float* out) {
+                float sc, inv;
+                pow2_scale<10>(column_max(m), sc, inv);
 #pragma unroll
-            for (int i = 0; i < 3; ++i) pow2_scale(column_max(m[i]), sc[i], inv[i]);
+                for (int s = 0; s < 2; ++s) {
 #pragma unroll
-            for (int s = 0; s < 2; ++s)
+                    for (int e = 0; e < 8; ++e) y[s][e] *= sc;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float y0 = x[0][s][e] * sc[0], y1 = x[1][s][e] * sc[1], y2 = x[2][s][e] * sc[2];
-                    opC.hi[s][e] = (_Float16)y0;
-                    opT.hi[s][e] = (_Float16)y1;
-                    opZ.hi[s][e] = (_Float16)y2;
+                    for (int e = 0; e < 8; ++e) op.hi[s][e] = (_Float16)y[s][e];
                     if (P == 2) {
-                        opC.lo[s][e] = (_Float16)(y0 - (float)opC.hi[s][e]);
-                        opT.lo[s][e] = (_Float16)(y1 - (float)opT.hi[s][e]);
-                        opZ.lo[s][e] = (_Float16)(y2 - (float)opZ.hi[s][e]);
+                        op.hi[s] = fixed_half(op.hi[s]);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) op.lo[s][e] = (_Float16)(y[s][e] - (float)op.hi[s][e]);
                     }
                 }
-            if (gq == 0) {
-                s_ic[row] = inv[0];
-                s_it[row] = inv[1];
-                s_iz[row] = inv[2];
-            }
+                if (gq == 0) out[row] = inv;  // both halves of the key channels write the same
+            };
+            convert(x[0], m[0], opC, s_ic);
+            convert(x[1], m[1], opT, s_it);
+            convert(x[2], m[2], opZ, s_iz);
         }
-        wave_lds_fence();
+        __syncthreads();
 
         // products over the value columns, and the small ones, per 16 key channels
-        float topS, topY, topD;
-        const Operand<P, VS> goS = operand(load_dO(), iS, nullptr, topS),
-                             yeS = operand(load_kept(Y), iY, iS, topY),
-                             eeD = operand(load_kept(E), iE, iD, topD);
-        float rq[4], rk[4], rt[4], ic[4], it[4], iz[4], qi[4], ki[4];
-        float reads[4] = {0.f, 0.f, 0.f, 0.f}, writes[4] = {0.f, 0.f, 0.f, 0.f}, dot = 0.f;
+        float reads[4] = {0.f, 0.f, 0.f, 0.f}, writes[4] = {0.f, 0.f, 0.f, 0.f};
+        float rq[4], rk[4], rt[4];
         const double l_end = s_l[GC - 1];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int t = 16 * w + 4 * gq + r;
             const float dec = __builtin_amdgcn_exp2f((float)s_l[t]);
-            rq[r] = a.scale * dec * (s_ri[t] * topS);
-            rk[r] = -dec * s_be[t] * topY;
-            rt[r] = __builtin_amdgcn_exp2f((float)(l_end - s_l[t])) * s_be[t] * topD;
-            ic[r] = s_ic[t];
-            it[r] = s_it[t];
-            iz[r] = s_iz[t];
-            qi[r] = pow2_inverse(fac[F_QS * GC + t]);
-            ki[r] = pow2_inverse(fac[F_KS * GC + t]);
+            rq[r] = a.scale * dec * (s_ri[t] * s_top[FOLD_S]);
+            rk[r] = -dec * s_be[t] * s_top[FOLD_YS];
+            rt[r] = __builtin_amdgcn_exp2f((float)(l_end - s_l[t])) * s_be[t] * s_top[FOLD_ED];
         }
+        // q or k of the result tile's places: four tokens of a channel
+        auto four = [&](int o, int k, float* y) {
+            const int b = w, rot = ((k >> 1) + KS * b) & 3;
+            const char* p = lds + o + (b * KS + (k >> 1)) * 1024 + (k & 1) * 8 + (li & 3) * 256 +
+                            ((4 * gq + (li >> 2) + rot) & 15) * 16;
+            const half4 x = lds_read_tr(p);
+            half4 z = x;
+            if (P == 2) z = lds_read_tr(p + Sh::RB);
 #pragma unroll
-        for (int k = 0; k < Sh::KT; ++k) {
-            floatx4 p1 = zero4(), p2 = zero4(), p3 = zero4();
+            for (int r = 0; r < 4; ++r) y[r] = (float)x[r] + (P == 2 ? (float)z[r] : 0.f);
+        };
+        {
+            const Operand<P, VS> goS = folded(go, FOLD_S), yeS = folded(ye, FOLD_YS);
 #pragma unroll
-            for (int s = 0; s < VS; ++s) {
-                const half8 sh = kept_row(S, 16 * k + li, s), dh = kept_row(dS, 16 * k + li, s);
-                half8 sl = sh, dl = dh;
-                if (P == 2) {
-                    sl = kept_row(S + DK * DVP, 16 * k + li, s);
-                    dl = kept_row(dS + DK * DVP, 16 * k + li, s);
+            for (int j = 0; j < KH; ++j) {
+                const int k = half * KH + j;
+                if (k >= KT) continue;
+                floatx4 p1 = zero4(), p2 = zero4();
+#pragma unroll
+                for (int s = 0; s < VS; ++s) {
+                    const half8 sh = state_frag(reg, k, s);
+                    half8 sl = sh;
+                    if (P == 2) sl = state_frag(reg + Ls::STATE / 2, k, s);
+                    p1 = mma_parts<P>(goS.hi[s], goS.lo[P == 2 ? s : 0], sh, sl, p1);
+                    p2 = mma_parts<P>(yeS.hi[s], yeS.lo[P == 2 ? s : 0], sh, sl, p2);
                 }
-                p1 = mma_parts<P>(goS.hi[s], goS.lo[P == 2 ? s : 0], sh, sl, p1);
-                p2 = mma_parts<P>(yeS.hi[s], yeS.lo[P == 2 ? s : 0], sh, sl, p2);
-                p3 = mma_parts<P>(eeD.hi[s], eeD.lo[P == 2 ? s : 0], dh, dl, p3);
-                if (k % 4 == w) {  // <S, dS>
-                    float y0 = 0.f, y1 = 0.f;
+                floatx4 a1 = zero4(), a2 = zero4(), a3 = zero4();
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        float x = (float)sh[e], y = (float)dh[e];
-                        if (P == 2) {
-                            x += (float)sl[e];
-                            y += (float)dl[e];
+                for (int s = 0; s < 2; ++s) {
+                    auto cols = [&](int o) {  // frag_cols with k known at run time
+                        half4 x[2];
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            const int b = 2 * s + u, rot = ((k >> 1) + KS * b) & 3;
+                            x[u] = lds_read_tr(lds + o + (b * KS + (k >> 1)) * 1024 + (k & 1) * 8 +
+                                               (li & 3) * 256 + ((4 * gq + (li >> 2) + rot) & 15) * 16);
                         }
-                        (e < 4 ? y0 : y1) += x * y;
+                        return __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7);
+                    };
+                    const half8 kh = cols(Sh::O_K), qh = cols(Sh::O_Q);
+                    half8 kl = kh, ql = qh;
+                    if (P == 2) {
+                        kl = cols(Sh::O_K + Sh::RB);
+                        ql = cols(Sh::O_Q + Sh::RB);
                     }
-                    dot += y0 * iS[2 * s] * iD[2 * s] + y1 * iS[2 * s + 1] * iD[2 * s + 1];
+                    a1 = mma_parts<P>(opC.hi[s], opC.lo[P == 2 ? s : 0], kh, kl, a1);
+                    a2 = mma_parts<P>(opT.hi[s], opT.lo[P == 2 ? s : 0], qh, ql, a2);
+                    a3 = mma_parts<P>(opZ.hi[s], opZ.lo[P == 2 ? s : 0], kh, kl, a3);
+                }
+                float qv[4], kv[4];
+                four(Sh::O_Q, k, qv);
+                four(Sh::O_K, k, kv);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int t = 16 * w + 4 * gq + r;
+                    const float x1 = rq[r] * p1[r], x2 = rk[r] * p2[r];
+                    reads[r] += (qv[r] * s_qs[t]) * x1 + (kv[r] * s_ks[t]) * x2;
+                    dq[j][r] += x1 + a1[r] * s_ic[t];
+                    dk[j][r] += x2 + (a2[r] * s_it[t] + a3[r] * s_iz[t]);
                 }
             }
-            floatx4 a1 = zero4(), a2 = zero4(), a3 = zero4();
+        }
+        if (!Ls::BOTH) {
+            __syncthreads();
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                const half8 kh = frag_ld(lds + Sh::O_KT, 2 * k + s, lane);
-                const half8 qh = frag_ld(lds + Sh::O_QT, 2 * k + s, lane);
-                half8 kl = kh, ql = qh;
-                if (P == 2) {
-                    kl = frag_ld(lds + Sh::O_KT + Sh::CB, 2 * k + s, lane);
-                    ql = frag_ld(lds + Sh::O_QT + Sh::CB, 2 * k + s, lane);
+            for (int j = 0; j < SP; ++j) {
+                const int i = tid + NT * j;
+                if (i < Ls::STATE / 16) reinterpret_cast<uint4*>(reg)[i] = bD[j];
+            }
+            __syncthreads();
+        }
+        {
+            const char* D = Ls::BOTH ? reg + Ls::STATE : reg;
+            const Operand<P, VS> eeD = folded(ee, FOLD_ED);
+#pragma unroll
+            for (int j = 0; j < KH; ++j) {
+                const int k = half * KH + j;
+                if (k >= KT) continue;
+                floatx4 p3 = zero4();
+#pragma unroll
+                for (int s = 0; s < VS; ++s) {
+                    const half8 dh = state_frag(D, k, s);
+                    half8 dl = dh;
+                    if (P == 2) dl = state_frag(D + Ls::STATE / 2, k, s);
+                    p3 = mma_parts<P>(eeD.hi[s], eeD.lo[P == 2 ? s : 0], dh, dl, p3);
                 }
-                if (s <= w / 2) a1 = mma_parts<P>(opC.hi[s], opC.lo[P == 2 ? s : 0], kh, kl, a1);
-                if (s >= w / 2) a2 = mma_parts<P>(opT.hi[s], opT.lo[P == 2 ? s : 0], qh, ql, a2);
-                a3 = mma_parts<P>(opZ.hi[s], opZ.lo[P == 2 ? s : 0], kh, kl, a3);
-            }
-            // q and k of the result tile's places: four tokens of a channel
-            const int at = frag_at(16 * k + li, 16 * w + 4 * gq, 2) * 2;
-            const half4 qh = *reinterpret_cast<const half4*>(lds + Sh::O_QT + at);
-            const half4 kh = *reinterpret_cast<const half4*>(lds + Sh::O_KT + at);
-            half4 ql = qh, kl = kh;
-            if (P == 2) {
-                ql = *reinterpret_cast<const half4*>(lds + Sh::O_QT + Sh::CB + at);
-                kl = *reinterpret_cast<const half4*>(lds + Sh::O_KT + Sh::CB + at);
-            }
+                float kv[4];
+                four(Sh::O_K, k, kv);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float qv = ((float)qh[r] + (P == 2 ? (float)ql[r] : 0.f)) * qi[r];
-                const float kv = ((float)kh[r] + (P == 2 ? (float)kl[r] : 0.f)) * ki[r];
-                const float x1 = rq[r] * p1[r], x2 = rk[r] * p2[r], x3 = rt[r] * p3[r];
-                reads[r] += qv * x1 + kv * x2;
-                writes[r] += kv * x3;
-                dq[k][r] += x1 + a1[r] * ic[r];
-                dk[k][r] += (x2 + x3) + (a2[r] * it[r] + a3[r] * iz[r]);
+                for (int r = 0; r < 4; ++r) {
+                    const float x3 = rt[r] * p3[r];
+                    writes[r] += (kv[r] * s_ks[16 * w + 4 * gq + r]) * x3;
+                    dk[j][r] += x3;
+                }
             }
         }
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const float x = row16_sum(reads[r]), y = row16_sum(writes[r]);
             if (li == 0) {
-                s_reads[16 * w + 4 * gq + r] = x;
-                s_writes[16 * w + 4 * gq + r] = y;
-            }
-        }
-        dot = wave_sum(dot);
-        if (lane == 0) s_dot[w] = dot;
-        if (tid < GC) {  // sums along P's rows, of what stands before each place
-            float f = 0.f;
-            for (int s = 0; s < GC; ++s) {
-                const float x = sP[tid * CP + s];
-                sP[tid * CP + s] = f;
-                f += x;
+                s_reads[half][16 * w + 4 * gq + r] = x;
+                s_writes[half][16 * w + 4 * gq + r] = y;
             }
         }
         __syncthreads();
-        if (w == 0) {  // lane = token
-            float after = s_reads[lane], before = s_writes[lane];
+        if (wave == 0) {  // lane = token
+            float after = s_reads[0][lane] + s_reads[1][lane], before = s_writes[0][lane] + s_writes[1][lane];
+            float tot = s_tot[lane];
 #pragma unroll
             for (int off = 1; off < 64; off <<= 1) {
                 const float x = __shfl_down(after, off, 64), y = __shfl_up(before, off, 64);
-                if (lane + off < 64) after += x;
+                const float z = __shfl_down(tot, off, 64);
+                if (lane + off < 64) {
+                    after += x;
+                    tot += z;
+                }
                 if (lane >= off) before += y;
             }
             before = __shfl_up(before, 1, 64);  // of the tokens before this one
             if (lane == 0) before = 0.f;
-            float cross = 0.f;  // down the columns, from the diagonal
-            for (int t = 0; t < GC; ++t) cross += t >= lane ? sP[t * CP + lane] : 0.f;
-            const float whole = gamma * ((s_dot[0] + s_dot[1]) + (s_dot[2] + s_dot[3]));
-            const float dlog = cross + after + before + whole;
+            float cross = lane >= 32 ? tot : 0.f;  // the column blocks of the other half
+            for (int b = 0; b < 4; ++b) cross += s_cross[b][lane];
+            float whole = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) whole += s_dot[i];
+            const float dlog = cross + after + before + fac[REC_FACTORS] * whole;
             if (lane < len) {
                 const size_t at = (size_t)(c0 + lane) * a.H + h;
                 ga.dalpha[at] = from_f32<T>(dlog / fmaxf(to_f32(a.alpha[at]), 0x1p-100f));
@@ -649,16 +891,19 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) void gdr_grad_kernel(c
         __syncthreads();
     }
 #pragma unroll
-    for (int k = 0; k < Sh::KT; ++k)
+    for (int j = 0; j < KH; ++j) {
+        const int k = half * KH + j;
+        if (k >= KT) continue;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int t = 16 * w + 4 * gq + r;
             if (t < len) {
                 const size_t at = ((size_t)(c0 + t) * a.Hk + hk) * DK + 16 * k + li;
-                ga.dq[at] = from_f32<T>(dq[k][r]);
-                ga.dk[at] = from_f32<T>(dk[k][r]);
+                ga.dq[at] = from_f32<T>(dq[j][r]);
+                ga.dk[at] = from_f32<T>(dk[j][r]);
             }
         }
+    }
 }
 
 template <class T, int DK, int DV, int NCW, int NLW>
@@ -671,7 +916,7 @@ hipError_t launch_rest(const GradArgs<T>& ga, hipStream_t stream)
                        stream, ga);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((gdr_grad_kernel<T, DK, DV>), dim3((unsigned)(a.maxch * a.Hk)), dim3(256), 0,
+    hipLaunchKernelGGL((gdr_grad_kernel<T, DK, DV>), dim3((unsigned)(a.maxch * a.Hk)), dim3(512), 0,
                        stream, ga);
     return hipGetLastError();
 }
@@ -695,14 +940,15 @@ struct Layout {
 template <class T>
 Layout layout(size_t units, int dk, int dv)
 {
-    const size_t dvp = dv < 32 ? 32 : dv, es = 2 * gdr_parts<T>();
+    const size_t es = 2 * gdr_parts<T>(), ks = dk < 32 ? 1 : dk / 32;
+    const size_t state = dv / 16 * ks * 512 * es, rows = dv / 16 * 1024 * es;
     Layout l;
     l.S = al256(units * gdr_rec_bytes<T, true>());
-    l.dS = l.S + al256(units * dk * dvp * es);
-    l.E = l.dS + al256(units * dk * dvp * es);
-    l.Y = l.E + al256(units * GC * dvp * es);
-    l.scale = l.Y + al256(units * GC * dvp * es);
-    l.total = l.scale + al256(units * KEEP_COUNT * (dv / 16) * 4);
+    l.dS = l.S + al256(units * state);
+    l.E = l.dS + al256(units * state);
+    l.Y = l.E + al256(units * rows);
+    l.scale = l.Y + al256(units * rows);
+    l.total = l.scale + al256(units * KEEP_COUNT * dv * 4);
     return l;
 }
 

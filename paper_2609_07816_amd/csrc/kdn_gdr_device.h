@@ -2,10 +2,10 @@
 // chunk geometry without a table.
 //
 // Numbers. A product of float32 accuracy on the 16-bit matrix instructions: each float32 operand x is
-// scaled by a power of two (exact) so that the largest value of its row or column lies in [2^14, 2^15),
-// and split x = hi + lo with hi = f16(x), lo = f16(x - hi): 22 bits, and values down to 2^-29 of the
-// largest keep all of them (f16 has subnormals down to 2^-24). hi hi + hi lo + lo hi then carries an
-// error of about 2^-22 of the row's and column's largest. A bf16 input needs no second half: its 8 bits
+// scaled by a power of two (exact) that brings the largest value of its row or column near 2^10, and
+// split x = hi + lo with hi = f16(x), lo = f16(x - hi): 22 bits for values down to 2^-12 of the largest,
+// and an error of 2^-34 of it below (f16 has subnormals down to 2^-24). hi hi + hi lo + lo hi then
+// carries an error of about 2^-22. A bf16 input needs no second half: its 8 bits
 // fit f16's 11 once its row is scaled. A float32 product of 16 columns costs 3 instructions of 16
 // cycles per 16x16x32 (2 with a bf16 input on one side) instead of 8 of 32 cycles on float32
 // instructions; bf16 halves would leave 2^-16.
@@ -34,13 +34,19 @@ __device__ __forceinline__ floatx4 mma(half8 a, half8 b, floatx4 c)
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
 
-// Power of two that brings m (the largest magnitude) into [2^14, 2^15), and its inverse. Below 2^-112
-// the scale stays at 2^126; infinities and NaN scale to themselves.
+// Power of two that brings m (the largest magnitude) into [2^TO, 2^(TO + 1)), and its inverse. The
+// exponent stays within the range of both; infinities and NaN scale to themselves.
+template <int TO = 14>
 __device__ __forceinline__ void pow2_scale(float m, float& sc, float& inv)
 {
-    const unsigned e = max((__float_as_uint(m) >> 23) & 255u, 15u);
-    sc = __uint_as_float((268u - e) << 23);
-    inv = __uint_as_float((e - 14u) << 23);
+    const unsigned e = min(max((__float_as_uint(m) >> 23) & 255u, TO + 1u), 253u);
+    sc = __uint_as_float((254u + TO - e) << 23);
+    inv = __uint_as_float((e - TO) << 23);
+}
+
+__device__ __forceinline__ float pow2_inverse(float x)  // of a power of two in [2^-126, 2^126]
+{
+    return __uint_as_float(0x7f000000u - __float_as_uint(x));
 }
 
 // Largest over the lanes that hold other rows of the same column (lanes 16 apart).
@@ -69,30 +75,43 @@ __device__ __forceinline__ float max_abs4(float m, const floatx4& x)
     return fmaxf(m, fmaxf(fabsf(x[2]), fabsf(x[3])));
 }
 
-// B fragment (halves hi and lo) of two result tiles stacked, scaled by sc.
+// B fragment (halves hi and lo) of two result tiles stacked.
 struct Split {
     half8 hi, lo;
 };
-__device__ __forceinline__ Split split(const floatx4& a, const floatx4& b, float sc)
-{
-    Split s;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const float x = a[j] * sc, y = b[j] * sc;
-        s.hi[j] = (_Float16)x;
-        s.hi[4 + j] = (_Float16)y;
-        s.lo[j] = (_Float16)(x - (float)s.hi[j]);
-        s.lo[4 + j] = (_Float16)(y - (float)s.hi[4 + j]);
-    }
-    return s;
-}
-__device__ __forceinline__ half8 to_half(const floatx4& a, const floatx4& b, float sc)
+__device__ __forceinline__ half8 to_half(const floatx4& a, const floatx4& b)
 {
     half8 s;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        s[j] = (_Float16)(a[j] * sc);
-        s[4 + j] = (_Float16)(b[j] * sc);
+        s[j] = (_Float16)a[j];
+        s[4 + j] = (_Float16)b[j];
+    }
+    return s;
+}
+// One value for the two uses of a hi half. Without it the compiler may round a product to f16 once from
+// its float32 value and once, for the subtraction, from the exact product, and the two differ where the
+// first rounding meets a tie of the second (about one value in 2^13).
+__device__ __forceinline__ half8 fixed_half(half8 x)
+{
+    uintx4 u = __builtin_bit_cast(uintx4, x);
+    asm("" : "+v"(u));
+    return __builtin_bit_cast(half8, u);
+}
+__device__ __forceinline__ half4 fixed_half(half4 x)
+{
+    uint64_t u = __builtin_bit_cast(uint64_t, x);
+    asm("" : "+v"(u));
+    return __builtin_bit_cast(half4, u);
+}
+__device__ __forceinline__ Split split(const floatx4& a, const floatx4& b)
+{
+    Split s;
+    s.hi = fixed_half(to_half(a, b));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        s.lo[j] = (_Float16)(a[j] - (float)s.hi[j]);
+        s.lo[4 + j] = (_Float16)(b[j] - (float)s.hi[4 + j]);
     }
     return s;
 }
@@ -208,24 +227,72 @@ __device__ __forceinline__ half8 frag_ld(const char* base, int frag, int lane)
     return *reinterpret_cast<const half8*>(base + frag * 1024 + lane * 16);
 }
 
-// LDS of one chunk: fragment-order K, K transposed, Q, Q transposed (each if wanted, P parts), then the
-// record's head and the part of its matrices that the kernel uses.
-template <class T, int DK, bool KR, bool KC, bool QR, bool QC, int MATS>
+// K and Q of a chunk in LDS: fragments (row block b, columns 32 s ..) of 1 KB, each 16 bytes of it (row
+// i, lane group g) at g * 256 + ((i + rot) & 15) * 16 with rot = (s + KSTEPS b) & 3, so that the loader's
+// lanes, which hold eight channels of four rows each, write to all banks. Read by rows (16 bytes of a
+// lane) or transposed (the hardware's transposing read of 4 x 16 values per group of 16 lanes).
+template <int KSTEPS>
+constexpr int frag_rot(int b, int s)
+{
+    return (s + KSTEPS * b) & 3;
+}
+
+struct LaneOffsets {  // of the four rotations
+    int row[4], tr[4];
+
+    __device__ __forceinline__ explicit LaneOffsets(int lane)
+    {
+        const int g = lane >> 4, i = lane & 15;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            row[r] = g * 256 + ((i + r) & 15) * 16;
+            tr[r] = (i & 3) * 256 + ((4 * g + (i >> 2) + r) & 15) * 16;
+        }
+    }
+};
+
+__device__ __forceinline__ half4 lds_read_tr(const char* p)
+{
+    typedef short short4v __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(
+        half4, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                   (__attribute__((address_space(3))) short4v*)(const_cast<char*>(p))));
+}
+
+// Rows 16b .. of the matrix, columns 32s ..
+template <int KSTEPS>
+__device__ __forceinline__ half8 frag_rows(const char* m, const LaneOffsets& lo, int b, int s)
+{
+    return *reinterpret_cast<const half8*>(m + (b * KSTEPS + s) * 1024 +
+                                           lo.row[frag_rot<KSTEPS>(b, s)]);
+}
+// Four rows 16b + 4g .. of column 16k + i.
+template <int KSTEPS>
+__device__ __forceinline__ half4 frag_cols4(const char* m, const LaneOffsets& lo, int k, int b)
+{
+    return lds_read_tr(m + (b * KSTEPS + (k >> 1)) * 1024 + (k & 1) * 8 +
+                       lo.tr[frag_rot<KSTEPS>(b, k >> 1)]);
+}
+// Columns 16k .. as rows of the transposed matrix, its columns (the matrix's rows) 32t ..
+template <int KSTEPS>
+__device__ __forceinline__ half8 frag_cols(const char* m, const LaneOffsets& lo, int k, int t)
+{
+    const half4 x = frag_cols4<KSTEPS>(m, lo, k, 2 * t), y = frag_cols4<KSTEPS>(m, lo, k, 2 * t + 1);
+    return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// LDS of one chunk: K, Q (P parts each, Q if wanted), then the record's head and MATS of its matrices.
+template <class T, int DK, bool Q, int MATS>
 struct ChunkLds {
     static constexpr int P = gdr_parts<T>();
     static constexpr int KSTEPS = DK < 32 ? 1 : DK / 32;
     static constexpr int KT = DK / 16;
-    static constexpr int RB = 4 * KSTEPS * 1024;  // K or Q by rows, one part
-    static constexpr int CB = KT * 2 * 1024;      // transposed, one part
-    static constexpr int O_K = 0;
-    static constexpr int O_KT = O_K + (KR ? P * RB : 0);
-    static constexpr int O_Q = O_KT + (KC ? P * CB : 0);
-    static constexpr int O_QT = O_Q + (QR ? P * RB : 0);
-    static constexpr int O_REC = O_QT + (QC ? P * CB : 0);
+    static constexpr int RB = 4 * KSTEPS * 1024;  // one part of K or Q
+    static constexpr int O_K = 0, O_Q = P * RB, O_REC = O_Q + (Q ? P * RB : 0);
     static constexpr int REC = MATS < 0 ? 0 : REC_HEAD + MATS * TRI_BYTES;
     static constexpr int BYTES = O_REC + REC;
     static constexpr int NBUF = 2 * BYTES <= 160 * 1024 ? 2 : 1;
-    static constexpr bool kr = KR, kc = KC, qr = QR, qc = QC;
+    static constexpr bool q = Q;
 };
 
 // Four tokens x eight channels of K or Q as stored.
@@ -233,17 +300,6 @@ template <class T>
 struct Raw8 {
     uint4 x[4][sizeof(T) / 2];
 
-    __device__ __forceinline__ void load(const T* base, size_t step, int t, int len, bool on)
-    {
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int u = 0; u < (int)sizeof(T) / 2; ++u) {
-                x[r][u] = make_uint4(0, 0, 0, 0);
-                if (on && t + r < len)
-                    x[r][u] = reinterpret_cast<const uint4*>(base + (size_t)(t + r) * step)[u];
-            }
-    }
     __device__ __forceinline__ float value(int r, int e) const
     {
         const uint4& y = x[r][e / (16 / (int)sizeof(T))];
@@ -255,69 +311,74 @@ struct Raw8 {
             return __uint_as_float(e & 1 ? p & 0xFFFF0000u : p << 16);
         }
     }
-    // Scaled by row, part p (0: hi, 1: lo), to the row fragments and the transposed ones.
-    template <bool ROWS, bool COLS, int KSTEPS>
-    __device__ __forceinline__ void store(const float4& sc, int p, int t, int c, _Float16* rows,
-                                          _Float16* cols) const
+    // Scaled by row, to the fragments.
+    template <int KSTEPS, int P>
+    __device__ __forceinline__ void store(const float4& sc, int t, int c, char* out, int part) const
     {
         const float f[4] = {sc.x, sc.y, sc.z, sc.w};
-        _Float16 y[4][8];
+        const int s = c >> 5, b = t >> 4, rot = (s + KSTEPS * b) & 3;
+        char* at = out + (b * KSTEPS + s) * 1024 + ((c & 15) >> 2) * 256 + ((c >> 4) & 1) * 8;
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+        for (int r = 0; r < 4; ++r) {
+            char* p = at + (((t & 15) + r + rot) & 15) * 16;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float z = value(r, e) * f[r];
-                y[r][e] = (_Float16)z;
-                if (p == 1) y[r][e] = (_Float16)(z - (float)y[r][e]);
+            for (int u = 0; u < 2; ++u) {
+                half4 y, z;
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    v[e] = value(r, 4 * u + e) * f[r];
+                    y[e] = (_Float16)v[e];
+                }
+                if (P == 2) y = fixed_half(y);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) z[e] = (_Float16)(v[e] - (float)y[e]);
+                *reinterpret_cast<half4*>(p + u * 256) = y;
+                if (P == 2) *reinterpret_cast<half4*>(p + u * 256 + part) = z;
             }
-        if (ROWS)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-                    *reinterpret_cast<half4*>(rows + frag_at(t + r, c + 4 * u, KSTEPS)) =
-                        half4{y[r][4 * u], y[r][4 * u + 1], y[r][4 * u + 2], y[r][4 * u + 3]};
-        if (COLS)
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                *reinterpret_cast<half4*>(cols + frag_at(c + e, t, 2)) =
-                    half4{y[0][e], y[1][e], y[2][e], y[3][e]};
+        }
     }
 };
 
 // The loading side of a workgroup: NT threads bring a chunk from memory to registers, and from there
-// to LDS. SKIP: bytes of the record between its head and the matrices wanted.
+// to LDS. Rows past the sequence's end repeat its last one, with a scale of 0 in the record: no load
+// stands in a branch. SKIP: bytes of the record between its head and the matrices wanted.
 template <class T, int DK, class Lds, int NT, int SKIP>
 struct Loader {
     static constexpr int TASKS = 2 * DK;  // (4 tokens, 8 channels) pieces of K, or of Q
     static constexpr int TPT = (TASKS + NT - 1) / NT;
     static constexpr int RECP = (Lds::REC / 16 + NT - 1) / NT;
-    static constexpr bool useq = Lds::qr || Lds::qc;
-    Raw8<T> k[TPT], q[useq ? TPT : 1];
-    float4 ks[TPT], qs[useq ? TPT : 1];  // the rows' scales
+    Raw8<T> k[TPT], q[Lds::q ? TPT : 1];
+    float4 ks[TPT], qs[Lds::q ? TPT : 1];  // the rows' scales
     uint4 rec[RECP > 0 ? RECP : 1];
 
-    __device__ __forceinline__ void load(const T* kbase, const T* qbase, size_t step, int tid, int len,
-                                         const char* recp)
+    // step: bytes of a token's row over all key heads
+    __device__ __forceinline__ void load(const T* kbase, const T* qbase, unsigned step, int tid,
+                                         int len, const char* recp)
     {
+        const float* fac = reinterpret_cast<const float*>(recp);
 #pragma unroll
         for (int j = 0; j < TPT; ++j) {
-            const int task = tid + NT * j, t = 4 * (task / (DK / 8) % 16), c = 8 * (task % (DK / 8));
-            const bool on = TASKS % NT == 0 || task < TASKS;
-            const float* fac = reinterpret_cast<const float*>(recp);
+            const int task = (tid + NT * j) % TASKS, t = 4 * (task / (DK / 8)), c = 8 * (task % (DK / 8));
             ks[j] = ld4(fac + F_KS * GC + t);
-            k[j].load(kbase + c, step, t, len, on);
-            if (useq) {
-                qs[j] = ld4(fac + F_QS * GC + t);
-                q[j].load(qbase + c, step, t, len, on);
+            if (Lds::q) qs[j] = ld4(fac + F_QS * GC + t);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const unsigned at = (unsigned)min(t + r, len - 1) * step + (unsigned)(c * sizeof(T));
+#pragma unroll
+                for (int u = 0; u < (int)sizeof(T) / 2; ++u) {
+                    k[j].x[r][u] = *reinterpret_cast<const uint4*>(
+                        reinterpret_cast<const char*>(kbase) + at + 16 * u);
+                    if (Lds::q)
+                        q[j].x[r][u] = *reinterpret_cast<const uint4*>(
+                            reinterpret_cast<const char*>(qbase) + at + 16 * u);
+                }
             }
         }
 #pragma unroll
         for (int j = 0; j < RECP; ++j) {
-            const int at = tid + NT * j;
-            if (at < Lds::REC / 16)
-                rec[j] = reinterpret_cast<const uint4*>(
-                    recp + (at < REC_HEAD / 16 ? 0 : SKIP))[at];
+            const int at = min(tid + NT * j, Lds::REC / 16 - 1);
+            rec[j] = reinterpret_cast<const uint4*>(recp + (at < REC_HEAD / 16 ? 0 : SKIP))[at];
         }
     }
 
@@ -325,36 +386,58 @@ struct Loader {
     {
 #pragma unroll
         for (int j = 0; j < TPT; ++j) {
-            const int task = tid + NT * j, t = 4 * (task / (DK / 8)), c = 8 * (task % (DK / 8));
-            if (TASKS % NT != 0 && task >= TASKS) break;
-#pragma unroll
-            for (int p = 0; p < Lds::P; ++p) {
-                k[j].template store<Lds::kr, Lds::kc, Lds::KSTEPS>(
-                    ks[j], p, t, c, reinterpret_cast<_Float16*>(buf + Lds::O_K + p * Lds::RB),
-                    reinterpret_cast<_Float16*>(buf + Lds::O_KT + p * Lds::CB));
-                if (useq)
-                    q[j].template store<Lds::qr, Lds::qc, Lds::KSTEPS>(
-                        qs[j], p, t, c, reinterpret_cast<_Float16*>(buf + Lds::O_Q + p * Lds::RB),
-                        reinterpret_cast<_Float16*>(buf + Lds::O_QT + p * Lds::CB));
-            }
+            const int task = (tid + NT * j) % TASKS, t = 4 * (task / (DK / 8)), c = 8 * (task % (DK / 8));
+            k[j].template store<Lds::KSTEPS, Lds::P>(ks[j], t, c, buf + Lds::O_K, Lds::RB);
+            if (Lds::q) q[j].template store<Lds::KSTEPS, Lds::P>(qs[j], t, c, buf + Lds::O_Q, Lds::RB);
         }
 #pragma unroll
         for (int j = 0; j < RECP; ++j)
-            if (tid + NT * j < Lds::REC / 16)
-                reinterpret_cast<uint4*>(buf + Lds::O_REC)[tid + NT * j] = rec[j];
+            reinterpret_cast<uint4*>(buf + Lds::O_REC)[min(tid + NT * j, Lds::REC / 16 - 1)] = rec[j];
     }
 };
 
-// Column of 16 values x four row blocks of [tokens][H][DV] in the layout of result tiles, as stored.
-template <class T>
-__device__ __forceinline__ void load_tile(const T* p, size_t step, int gq, int len, T* x)
+// Byte offsets of a lane's 16 places of a chunk's column (result tile layout) from the chunk's first
+// token: rows past the end repeat the last one. step: bytes of a token's row, at: of this lane's column.
+__device__ __forceinline__ void tile_offsets(unsigned step, unsigned at, int gq, int len, unsigned* off)
 {
 #pragma unroll
     for (int b = 0; b < 4; ++b)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-            x[4 * b + r] = p[(size_t)min(16 * b + 4 * gq + r, len - 1) * step];
+            off[4 * b + r] = (unsigned)min(16 * b + 4 * gq + r, len - 1) * step + at;
 }
+// Values kept as loaded, a register each (a bf16 zero-extended): packed two to a register, they would be
+// waited for at once.
+template <class T>
+__device__ __forceinline__ void load_tile(const T* p, const unsigned* off, typename Raw1<T>::type* x)
+{
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const char* at = reinterpret_cast<const char*>(p) + off[i];
+        if constexpr (sizeof(T) == 2)
+            x[i] = *reinterpret_cast<const unsigned short*>(at);
+        else
+            x[i] = *reinterpret_cast<const float*>(at);
+    }
+}
+// Stores of a chunk of len tokens: whole chunks without a branch per row.
+template <class T>
+__device__ __forceinline__ void store_tile(T* p, const unsigned* off, int gq, int len, const T* x)
+{
+    if (len == GC) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) *reinterpret_cast<T*>(reinterpret_cast<char*>(p) + off[i]) = x[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (16 * (i >> 2) + 4 * gq + (i & 3) < len)
+                *reinterpret_cast<T*>(reinterpret_cast<char*>(p) + off[i]) = x[i];
+    }
+}
+
+// Keeps what stands before it (requests of operands) before what stands after it (the products and
+// conversions that their latency hides behind).
+__device__ __forceinline__ void request_fence() { __builtin_amdgcn_sched_barrier(0); }
 
 __device__ __forceinline__ void unpack4(const float4& x, float* y)
 {

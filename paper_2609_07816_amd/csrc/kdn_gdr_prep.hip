@@ -180,10 +180,10 @@ __global__ __launch_bounds__(256) void gdr_prep_kernel(const ChunkArgs<T> a)
                 const float z[4] = {y[j].x * sc, y[j].y * sc, y[j].z * sc, y[j].w * sc};
                 half4 p, q;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    p[e] = (_Float16)z[e];
-                    q[e] = (_Float16)(z[e] - (float)p[e]);
-                }
+                for (int e = 0; e < 4; ++e) p[e] = (_Float16)z[e];
+                p = fixed_half(p);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) q[e] = (_Float16)(z[e] - (float)p[e]);
                 *reinterpret_cast<half4*>(at + 16 * 8 * j) = p;
                 if (lo) *reinterpret_cast<half4*>(lo + (at - hi) + 16 * 8 * j) = q;
             }
@@ -253,11 +253,11 @@ __global__ __launch_bounds__(256) void gdr_prep_kernel(const ChunkArgs<T> a)
     if (gq == 0) {
         const int t = 16 * w + li;
         float ks, ki, qs, qi;
-        pow2_scale(mk, ks, ki);
-        pow2_scale(mq, qs, qi);
+        pow2_scale<0>(mk, ks, ki);  // the largest in [1, 2): f16 keeps 2^-25 of it
+        pow2_scale<0>(mq, qs, qi);
         const float dec = __builtin_amdgcn_exp2f((float)s_l[t]);
-        fac[F_KS * GC + t] = ks;
-        fac[F_QS * GC + t] = qs;
+        fac[F_KS * GC + t] = t < len ? ks : 0.f;  // what stands past the end counts as 0
+        fac[F_QS * GC + t] = t < len ? qs : 0.f;
         fac[F_G1 * GC + t] = dec * ki;
         fac[F_W * GC + t] = __builtin_amdgcn_exp2f((float)(l_end - s_l[t])) * ki;
         fac[F_GQ * GC + t] = dec * a.scale * qi;

@@ -6,30 +6,48 @@
 //
 // A workgroup has 16 NCW value columns of one (sequence, head). Its NCW chain waves carry 16 columns
 // each, S in registers, and exchange nothing; NLW loader waves bring the next chunk's K and Q (scaled,
-// f16, fragment order; K also transposed), matrices and factors into the other LDS buffer. One barrier
-// per chunk. For the backward (BWD) it writes each chunk's entering S and E in place of O.
+// f16, fragment order), matrices and factors into the other LDS buffer. One barrier per chunk. For the
+// backward (BWD) it keeps each chunk's entering S and E in place of O.
 #pragma once
 
 #include "kdn_gdr_device.h"
 
 namespace kdn {
 
-// What the backward keeps of every chunk and head, beside the records: the state S entering it and
-// the adjoint dS of the state leaving it [dk][dvp], its innovations E and the adjoint Y of its writes
-// [64][dvp] as f16 (float32 calls: a second plane with the low halves), each 16-column tile scaled by a
-// power of two, whose inverses are in `scale` [4][dv / 16]. Columns stand in the order in which a lane
-// of a fragment holds them (col_place), dvp = max(dv, 32).
+// What the backward keeps of every chunk and head, beside the records: the state S entering it and the
+// adjoint dS of the state leaving it, its innovations E and the adjoint Y of its writes, as f16 (float32
+// calls: a second plane with the low halves) in the order in which the walks hold them: for each 16 value
+// columns the fragments of 32 key channels (S, dS) or tokens (E, Y), 16 bytes of a lane. Every value
+// column is scaled by a power of two, whose inverses are in `scale` [4][dv].
 struct GdrKeep {
     _Float16 *S, *dS, *E, *Y;
     float* scale;
 };
 enum { KEEP_S, KEEP_E, KEEP_DS, KEEP_Y, KEEP_COUNT };
-
-__device__ __forceinline__ int col_place(int n)
+template <class T, int DK>
+constexpr size_t keep_state(int dv)  // values of S or dS of one chunk and head
 {
-    return (n & ~31) + ((n & 15) >> 2) * 8 + (n & 3) + ((n >> 4) & 1) * 4;
+    return (size_t)(dv / 16) * (DK < 32 ? 1 : DK / 32) * 512 * gdr_parts<T>();
+}
+template <class T>
+constexpr size_t keep_rows(int dv)  // of E or Y
+{
+    return (size_t)(dv / 16) * 1024 * gdr_parts<T>();
 }
 
+// Scales of a column of values that a chain keeps in range of f16: by s, whose inverse is i.
+struct ColScale {
+    float s, i;
+
+    // For values whose largest is m (scaled by s): a new scale that brings it near 2^10, and the factor
+    // to apply to what is scaled by the old one.
+    __device__ __forceinline__ float renew(float m)
+    {
+        const float old = i;
+        pow2_scale<10>(m * i, s, i);
+        return s * old;
+    }
+};
 __device__ __forceinline__ float wave_max(float x)  // of values that are not negative
 {
     unsigned u = __float_as_uint(x);
@@ -46,42 +64,25 @@ __device__ __forceinline__ float wave_max(float x)  // of values that are not ne
     return __uint_as_float((unsigned)__builtin_amdgcn_readlane((int)u, 63));
 }
 
-// A wave's 16 columns of a kept matrix (NB row blocks of result tiles), and their inverse scale.
-template <int P, int DV, int NB>
-__device__ __forceinline__ void keep_tile(_Float16* out, float* inv_out, const floatx4* x, int col,
-                                          int gq)
+constexpr float COL_TOP = 60000.f;  // below f16's largest value, 65504
+__device__ __forceinline__ bool too_large(float m) { return m > COL_TOP && m < INFINITY; }
+
+__device__ __forceinline__ floatx4 scaled(const floatx4& x, float f)
 {
-    constexpr int DVP = DV < 32 ? 32 : DV;
-    float m = 0.f, sc, inv;
-#pragma unroll
-    for (int b = 0; b < NB; ++b) m = max_abs4(m, x[b]);
-    pow2_scale(wave_max(m), sc, inv);
-    _Float16* at = out + 4 * gq * DVP + col_place(col);
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const float z = x[b][r] * sc;
-            const _Float16 hi = (_Float16)z;
-            _Float16* p = at + (16 * b + r) * DVP;
-            p[0] = hi;
-            if (DV == 16) p[4] = (_Float16)0.f;
-            if (P == 2) {
-                p[NB * 16 * DVP] = (_Float16)(z - (float)hi);
-                if (DV == 16) p[NB * 16 * DVP + 4] = (_Float16)0.f;
-            }
-        }
-    if ((threadIdx.x & 63) == 0) *inv_out = inv;
+    return floatx4{x[0] * f, x[1] * f, x[2] * f, x[3] * f};
 }
 
+__device__ __forceinline__ void st8(_Float16* p, half8 x) { *reinterpret_cast<half8*>(p) = x; }
+
 template <class T, int DK, bool BWD>
-using WalkLds = ChunkLds<T, DK, true, true, !BWD, false, BWD ? 2 : 2 + gdr_parts<T>()>;
+using WalkLds = ChunkLds<T, DK, !BWD, BWD ? 2 : 2 + gdr_parts<T>()>;
 
 template <class T, int DK, int DV, int NCW, int NLW, bool BWD>
 __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_walk_kernel(const ChunkArgs<T> a,
                                                                     const GdrKeep keep)
 {
     using Sh = WalkLds<T, DK, BWD>;
+    constexpr int P = Sh::P, KS = Sh::KSTEPS, KT = Sh::KT;
     constexpr int REC = gdr_rec_bytes<T, BWD>();
     constexpr int TILES = DV / (16 * NCW);  // workgroups of a chain
     __shared__ __align__(16) char lds[Sh::NBUF * Sh::BYTES];
@@ -107,10 +108,10 @@ __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_walk_kernel(const ChunkA
     if (wave >= NCW) {
         const int tid = threadIdx.x - 64 * NCW;
         Loader<T, DK, Sh, 64 * NLW, 0> ld;
-        const size_t step = (size_t)a.Hk * DK;
         auto load = [&](int c) {
             const size_t at = ((size_t)(t0 + c * GC) * a.Hk + hk) * DK;
-            ld.load(a.k + at, a.q + at, step, tid, t1 - t0 - c * GC, rec0 + (size_t)c * rstep);
+            ld.load(a.k + at, a.q + at, (unsigned)(a.Hk * DK * sizeof(T)), tid,
+                    min(GC, t1 - t0 - c * GC), rec0 + (size_t)c * rstep);
         };
         if (nch > 0) {
             load(0);
@@ -129,183 +130,284 @@ __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_walk_kernel(const ChunkA
         return;
     }
 
-    const int col = (tile * NCW + wave) * 16 + li;
+    const int ctile = tile * NCW + wave, col = ctile * 16 + li;
     const size_t sbase = ((size_t)n * a.H + h) * DK * DV + (size_t)(4 * gq) * DV + col;
-    floatx4 S[Sh::KT];
-#pragma unroll
-    for (int k = 0; k < Sh::KT; ++k)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-            S[k][r] = a.S0 ? a.S0[sbase + (size_t)(16 * k + r) * DV] : 0.f;
-
-    const size_t vstep = (size_t)a.H * DV;
-    T vn[16];
+    const unsigned vstep = (unsigned)(a.H * DV * sizeof(T)), vcol = (unsigned)((h * DV + col) * sizeof(T));
+    auto vrow = [&](auto* p, int c) { return p + (size_t)(t0 + c * GC) * a.H * DV; };
+    unsigned off[16];
+    typename Raw1<T>::type vn[16];
     auto load_v = [&](int c) {
-        load_tile(a.v + ((size_t)(t0 + c * GC) * a.H + h) * DV + col, vstep, gq,
-                  min(GC, t1 - t0 - c * GC), vn);
+        const int len = t1 - t0 - c * GC;
+        if (len < GC) tile_offsets(vstep, vcol, gq, len, off);  // the last chunk
+        load_tile(vrow(a.v, c), off, vn);
     };
-    if (nch > 0) load_v(0);
+    floatx4 S[KT];  // scaled by sS
+    ColScale sS = {1.f, 1.f}, sU = {1.f, 1.f};
+    const LaneOffsets lo(lane);
+    {
+        float m = 0.f;
+#pragma unroll
+        for (int k = 0; k < KT; ++k) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                S[k][r] = a.S0 ? a.S0[sbase + (size_t)(16 * k + r) * DV] : 0.f;
+            m = max_abs4(m, S[k]);
+        }
+        tile_offsets(vstep, vcol, gq, GC, off);
+        if (nch > 0) load_v(0);
+        m = column_max(m);
+        float mv = m;
+        if (nch > 0)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) mv = fmaxf(mv, fabsf(Raw1<T>::f32(vn[i])));
+        mv = column_max(mv);
+        if (mv > 0.f && mv < INFINITY) sU.renew(mv);
+        sS = sU;
+        if (m > 0.f && m < INFINITY) sS.renew(m * sS.s);
+#pragma unroll
+        for (int k = 0; k < KT; ++k) S[k] = scaled(S[k], sS.s);
+    }
     __syncthreads();
     for (int c = 0; c < nch; ++c) {
         const char* buf = lds + c % Sh::NBUF * Sh::BYTES;
         const float* fac = reinterpret_cast<const float*>(buf + Sh::O_REC);
         const char* tri = buf + Sh::O_REC + REC_HEAD;
         const int len = min(GC, t1 - t0 - c * GC);
-        auto factor = [&](int f, int b) { return ld4(fac + f * GC + 16 * b + 4 * gq); };
-        float V[4][4];
+        auto factor = [&](int f, int b, float* x) { unpack4(ld4(fac + f * GC + 16 * b + 4 * gq), x); };
+        floatx4 V[4];
 #pragma unroll
         for (int b = 0; b < 4; ++b)
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                V[b][r] = 16 * b + 4 * gq + r < len ? to_f32(vn[4 * b + r]) : 0.f;
-        if (c + 1 < nch) load_v(c + 1);
+            for (int r = 0; r < 4; ++r) V[b][r] = Raw1<T>::f32(vn[4 * b + r]);
 
-        const size_t kept = (size_t)(g0 + c) * a.H + h;
-        constexpr int DVP = DV < 32 ? 32 : DV;
-        if (BWD)
-            keep_tile<Sh::P, DV, Sh::KT>(keep.S + kept * DK * DVP * Sh::P,
-                                         keep.scale + (kept * KEEP_COUNT + KEEP_S) * (DV / 16) + col / 16,
-                                         S, col, gq);
-
-        // S in halves
-        float m = 0.f, sc, s_inv;
+        float m = 0.f;
 #pragma unroll
-        for (int k = 0; k < Sh::KT; ++k) m = max_abs4(m, S[k]);
-        pow2_scale(column_max(m), sc, s_inv);
-        Split sp[Sh::KSTEPS];
+        for (int k = 0; k < KT; ++k) m = max_abs4(m, S[k]);
+        m = column_max(m);
+        if (__any(too_large(4.f * m) || (m < 16.f && m > 0.f))) {
+            const float f = too_large(4.f * m) || (m < 16.f && m > 0.f) ? sS.renew(m) : 1.f;
 #pragma unroll
-        for (int s = 0; s < Sh::KSTEPS; ++s)
-            sp[s] = split(S[2 * s], Sh::KT > 1 ? S[2 * s + 1] : zero4(), sc);
-
-        // K S and Q S
-        floatx4 x[4], o[4];
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            x[b] = zero4();
-            o[b] = zero4();
-#pragma unroll
-            for (int s = 0; s < Sh::KSTEPS; ++s) {
-                const half8 kf = frag_ld(buf + Sh::O_K, b * Sh::KSTEPS + s, lane);
-                x[b] = mma(kf, sp[s].hi, x[b]);
-                x[b] = mma(kf, sp[s].lo, x[b]);
-                if (Sh::P == 2)
-                    x[b] = mma(frag_ld(buf + Sh::O_K + Sh::RB, b * Sh::KSTEPS + s, lane), sp[s].hi,
-                               x[b]);
-                if (!BWD) {
-                    const half8 qf = frag_ld(buf + Sh::O_Q, b * Sh::KSTEPS + s, lane);
-                    o[b] = mma(qf, sp[s].hi, o[b]);
-                    if (Sh::P == 2) {
-                        o[b] = mma(qf, sp[s].lo, o[b]);
-                        o[b] = mma(frag_ld(buf + Sh::O_Q + Sh::RB, b * Sh::KSTEPS + s, lane),
-                                   sp[s].hi, o[b]);
-                    }
-                }
-            }
+            for (int k = 0; k < KT; ++k) S[k] = scaled(S[k], f);
         }
-        // X = V - 2^l K S, and beta X in halves
-        floatx4 bx[4];
-        m = 0.f;
+        Split sp[KS], ys[2], us[2];
+        floatx4 o[4], e[4];
+        half8 kc[KT][2];
+        float mu;
+        // Again with other scales where a column has left f16's range, which costs a chunk's time and
+        // hardly happens: the scales follow the columns. Ends at the latest when a scale cannot fall.
+        for (int tries = 0;; ++tries) {
+            half8 kf[KS][4];
+            float g1[4][4], be[4][4];
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            float g1[4], be[4];
-            unpack4(factor(F_G1, b), g1);
-            unpack4(factor(F_BE, b), be);
+            for (int s = 0; s < KS; ++s)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                x[b][r] = fmaf(-g1[r], x[b][r] * s_inv, V[b][r]);
-                bx[b][r] = be[r] * x[b][r];
-            }
-            m = max_abs4(m, bx[b]);
-        }
-        float x_inv;
-        pow2_scale(column_max(m), sc, x_inv);
-        const Split xs[2] = {split(bx[0], bx[1], sc), split(bx[2], bx[3], sc)};
-        // E = X - W (beta X), U = beta E
-        floatx4 u[4], y[4];
-        m = 0.f;
-        float mw = 0.f;
+                for (int b = 0; b < 4; ++b) kf[s][b] = frag_rows<KS>(buf + Sh::O_K, lo, b, s);
+            request_fence();
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            floatx4 d = zero4();
-#pragma unroll
-            for (int s = 0; s <= b / 2; ++s) {
-                const half8 wh = frag_ld(tri, tri_frag(b, s), lane);
-                d = mma(wh, xs[s].hi, d);
-                d = mma(wh, xs[s].lo, d);
-                d = mma(frag_ld(tri, TRI + tri_frag(b, s), lane), xs[s].hi, d);
-            }
-            float wr[4], w[4], be[4];
-            unpack4(factor(F_WR, b), wr);
-            unpack4(factor(F_W, b), w);
-            unpack4(factor(F_BE, b), be);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                x[b][r] = fmaf(-wr[r], d[r] * x_inv, x[b][r]);
-                u[b][r] = be[r] * x[b][r];
-                y[b][r] = w[r] * u[b][r];
-            }
-            m = max_abs4(m, u[b]);
-            mw = max_abs4(mw, y[b]);
-        }
-        if (BWD)
-            keep_tile<Sh::P, DV, 4>(keep.E + kept * GC * DVP * Sh::P,
-                                    keep.scale + (kept * KEEP_COUNT + KEEP_E) * (DV / 16) + col / 16, x,
-                                    col, gq);
-        // S <- 2^l_C S + K^T (2^(l_C - l) U)
-        float y_inv;
-        pow2_scale(column_max(mw), sc, y_inv);
-        const Split ys[2] = {split(y[0], y[1], sc), split(y[2], y[3], sc)};
-        const float gc = fac[REC_FACTORS];
-#pragma unroll
-        for (int k = 0; k < Sh::KT; ++k) {
-            floatx4 d = zero4();
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                const half8 kf = frag_ld(buf + Sh::O_KT, 2 * k + s, lane);
-                d = mma(kf, ys[s].hi, d);
-                d = mma(kf, ys[s].lo, d);
-                if (Sh::P == 2)
-                    d = mma(frag_ld(buf + Sh::O_KT + Sh::CB, 2 * k + s, lane), ys[s].hi, d);
-            }
-#pragma unroll
-            for (int r = 0; r < 4; ++r) S[k][r] = fmaf(gc, S[k][r], d[r] * y_inv);
-        }
-        if (!BWD) {  // O = scale (2^l Q S + A U)
-            float u_inv;
-            pow2_scale(column_max(m), sc, u_inv);
-            const Split us[2] = {split(u[0], u[1], sc), split(u[2], u[3], sc)};
-            T* op = a.o + ((size_t)(t0 + c * GC) * a.H + h) * DV + col;
+            for (int s = 0; s < KS; ++s) sp[s] = split(S[2 * s], KT > 1 ? S[2 * s + 1] : zero4());
+            request_fence();
+            // K S, then Q S beside X
+            floatx4 x[4];
+            half8 qf[KS][4];
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
-                floatx4 d = zero4();
+                factor(F_G1, b, g1[b]);
+                factor(F_BE, b, be[b]);
+                x[b] = zero4();
+                o[b] = zero4();
+            }
+            if (!BWD)
 #pragma unroll
-                for (int s = 0; s <= b / 2; ++s) {
-                    const half8 af = frag_ld(tri, 2 * TRI + tri_frag(b, s), lane);
-                    d = mma(af, us[s].hi, d);
-                    if (Sh::P == 2) {
-                        d = mma(af, us[s].lo, d);
-                        d = mma(frag_ld(tri, 3 * TRI + tri_frag(b, s), lane), us[s].hi, d);
+                for (int s = 0; s < KS; ++s)
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) qf[s][b] = frag_rows<KS>(buf + Sh::O_Q, lo, b, s);
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+#pragma unroll
+                for (int b = 0; b < 4; ++b) x[b] = mma(kf[s][b], sp[s].hi, x[b]);
+#pragma unroll
+                for (int b = 0; b < 4; ++b) x[b] = mma(kf[s][b], sp[s].lo, x[b]);
+                if (P == 2)
+#pragma unroll
+                    for (int b = 0; b < 4; ++b)
+                        x[b] = mma(frag_rows<KS>(buf + Sh::O_K + Sh::RB, lo, b, s), sp[s].hi, x[b]);
+            }
+            request_fence();
+            half8 wh[TRI], wl[TRI];
+#pragma unroll
+            for (int i = 0; i < TRI; ++i) {
+                wh[i] = frag_ld(tri, i, lane);
+                wl[i] = frag_ld(tri, TRI + i, lane);
+            }
+            if (!BWD)
+#pragma unroll
+                for (int s = 0; s < KS; ++s)
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) {
+                        o[b] = mma(qf[s][b], sp[s].hi, o[b]);
+                        if (P == 2) {
+                            o[b] = mma(qf[s][b], sp[s].lo, o[b]);
+                            o[b] = mma(frag_rows<KS>(buf + Sh::O_Q + Sh::RB, lo, b, s), sp[s].hi, o[b]);
+                        }
                     }
-                }
-                float gv[4], av[4];
-                unpack4(factor(F_GQ, b), gv);
-                unpack4(factor(F_AR, b), av);
+            // X = V - 2^l K S, and beta X in halves
+            floatx4 bx[4];
+            const float xs = sU.s * sS.i;
+            float mb = 0.f;
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int t = 16 * b + 4 * gq + r;
-                    const float z = fmaf(gv[r], o[b][r] * s_inv, av[r] * (d[r] * u_inv));
-                    if (t < len) op[(size_t)t * vstep] = from_f32<T>(z);
+                    x[b][r] = fmaf(V[b][r], sU.s, -g1[b][r] * (x[b][r] * xs));
+                    bx[b][r] = be[b][r] * x[b][r];
                 }
+                mb = max_abs4(mb, bx[b]);
+            }
+            const Split bs[2] = {split(bx[0], bx[1]), split(bx[2], bx[3])};
+            request_fence();
+            // E = X - W (beta X), U = beta E, and U over the rest of the chunk's decay
+            float wr[4][4], w[4][4];
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                factor(F_WR, b, wr[b]);
+                factor(F_W, b, w[b]);
+            }
+#pragma unroll
+            for (int k = 0; k < KT; ++k)
+#pragma unroll
+                for (int s = 0; s < 2; ++s) kc[k][s] = frag_cols<KS>(buf + Sh::O_K, lo, k, s);
+            floatx4 d[4];
+#pragma unroll
+            for (int b = 0; b < 4; ++b) d[b] = zero4();
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+#pragma unroll
+                for (int b = 2 * s; b < 4; ++b) d[b] = mma(wh[tri_frag(b, s)], bs[s].hi, d[b]);
+#pragma unroll
+                for (int b = 2 * s; b < 4; ++b) d[b] = mma(wh[tri_frag(b, s)], bs[s].lo, d[b]);
+#pragma unroll
+                for (int b = 2 * s; b < 4; ++b) d[b] = mma(wl[tri_frag(b, s)], bs[s].hi, d[b]);
+            }
+            request_fence();
+            floatx4 u[4], y[4];
+            const float yscale = sS.s * sU.i;
+            float my = 0.f;
+            mu = 0.f;
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    e[b][r] = fmaf(-wr[b][r], d[b][r], x[b][r]);
+                    u[b][r] = be[b][r] * e[b][r];
+                    y[b][r] = (w[b][r] * yscale) * u[b][r];
+                }
+                mu = max_abs4(mu, BWD ? e[b] : u[b]);
+                if (BWD) mu = max_abs4(mu, u[b]);
+                my = max_abs4(my, y[b]);
+            }
+            ys[0] = split(y[0], y[1]);
+            ys[1] = split(y[2], y[3]);
+            if (!BWD) {
+                us[0] = split(u[0], u[1]);
+                us[1] = split(u[2], u[3]);
+            }
+            if (!__any(too_large(mb) || too_large(mu) || too_large(my)) || tries == 8) break;
+            mb = column_max(mb);
+            mu = column_max(mu);
+            my = column_max(my);
+            float f = 1.f;
+            if (too_large(mb))
+                sU.renew(mb);
+            else if (too_large(mu))
+                sU.renew(mu);
+            else if (too_large(my))
+                f = sS.renew(my);
+#pragma unroll
+            for (int k = 0; k < KT; ++k) S[k] = scaled(S[k], f);
+        }
+        if (c + 1 < nch && t1 - t0 - (c + 1) * GC >= GC) load_tile(vrow(a.v, c + 1), off, vn);
+        if (BWD) {
+            const size_t kept = (size_t)(g0 + c) * a.H + h;
+            _Float16* ks = keep.S + kept * keep_state<T, DK>(DV) + (size_t)(ctile * KS * 64 + lane) * 8;
+            _Float16* ke = keep.E + kept * keep_rows<T>(DV) + (size_t)(ctile * 2 * 64 + lane) * 8;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                st8(ks + s * 512, sp[s].hi);
+                if (P == 2) st8(ks + (DV / 16 * KS + s) * 512, sp[s].lo);
+            }
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const Split x = split(e[2 * s], e[2 * s + 1]);
+                st8(ke + s * 512, x.hi);
+                if (P == 2) st8(ke + (DV / 16 * 2 + s) * 512, x.lo);
+            }
+            float* sc = keep.scale + kept * KEEP_COUNT * DV + col;
+            if (gq == 0) {
+                sc[KEEP_S * DV] = sS.i;
+                sc[KEEP_E * DV] = sU.i;
             }
         }
+        // S <- 2^l_C S + K^T (2^(l_C - l) U)
+        const float gc = fac[REC_FACTORS];
+        half8 af[TRI];
+        float gv[4][4], av[4][4];
+        if (!BWD) {
+#pragma unroll
+            for (int i = 0; i < TRI; ++i) af[i] = frag_ld(tri, 2 * TRI + i, lane);
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                factor(F_GQ, b, gv[b]);
+                factor(F_AR, b, av[b]);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < KT; ++k) S[k] = scaled(S[k], gc);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+#pragma unroll
+            for (int k = 0; k < KT; ++k) S[k] = mma(kc[k][s], ys[s].hi, S[k]);
+#pragma unroll
+            for (int k = 0; k < KT; ++k) S[k] = mma(kc[k][s], ys[s].lo, S[k]);
+            if (P == 2)
+#pragma unroll
+                for (int k = 0; k < KT; ++k)
+                    S[k] = mma(frag_cols<KS>(buf + Sh::O_K + Sh::RB, lo, k, s), ys[s].hi, S[k]);
+        }
+        if (!BWD) {  // O = scale (2^l Q S + A U)
+            floatx4 d[4];
+            T out[16];
+#pragma unroll
+            for (int b = 0; b < 4; ++b) d[b] = zero4();
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int b = 2 * s; b < 4; ++b) {
+                    d[b] = mma(af[tri_frag(b, s)], us[s].hi, d[b]);
+                    if (P == 2) {
+                        d[b] = mma(af[tri_frag(b, s)], us[s].lo, d[b]);
+                        d[b] = mma(frag_ld(tri, 3 * TRI + tri_frag(b, s), lane), us[s].hi, d[b]);
+                    }
+                }
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    out[4 * b + r] = from_f32<T>(
+                        fmaf(gv[b][r], o[b][r] * sS.i, av[b][r] * (d[b][r] * sU.i)));
+            store_tile(vrow(a.o, c), off, gq, len, out);
+        }
+        if (c + 1 < nch && t1 - t0 - (c + 1) * GC < GC) load_v(c + 1);  // the last chunk, not whole
+        // a column of writes that has become small gets its bits back
+        mu = column_max(mu);
+        if (mu < 4.f && mu > 0.f) sU.renew(mu);
         if (Sh::NBUF == 1) __syncthreads();
         __syncthreads();
     }
     if (a.S_T)
 #pragma unroll
-        for (int k = 0; k < Sh::KT; ++k)
+        for (int k = 0; k < KT; ++k)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) a.S_T[sbase + (size_t)(16 * k + r) * DV] = S[k][r];
+            for (int r = 0; r < 4; ++r) a.S_T[sbase + (size_t)(16 * k + r) * DV] = S[k][r] * sS.i;
 }
 
 template <bool BWD, class T, int DK, int DV, int NCW, int NLW>

@@ -39,6 +39,11 @@ def draw(seed, B, T, H, Hk, dk, dv, dtype="f32", N=None, state=False, gates="usu
         x["k"] = x["k"] * s
         x["q"] = x["q"] * 2.0 ** g.integers(-20, 20, (B, T, Hk, 1))
         x["v"] = x["v"] * 2.0 ** g.integers(-10, 10, (B, T, H, 1))
+    elif gates == "jumps":    # columns whose values change by up to 2^40 from one stretch to the next
+        x["alpha"] = np.full((B, T, H), 0.25)
+        for name in ("v", "dO"):
+            s = 2.0 ** g.integers(-20, 21, (B, T // 40 + 1, H, dv))
+            x[name] = x[name] * np.repeat(s, 40, axis=1)[:, :T]
     else:
         raise ValueError(gates)
     x = {n: (to_bf16(y) if dtype == "bf16" else y.astype(np.float32).astype(np.float64))

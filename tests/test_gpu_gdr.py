@@ -48,6 +48,7 @@ SHAPES = [
     (1, 150, 2, 1, 16, 128, True, "one"),
     (1, 190, 2, 2, 128, 16, True, "scaled"),
     (2, 333, 2, 2, 128, 128, False, "usual"),
+    (1, 300, 2, 1, 64, 64, True, "jumps"),
     ([0, 1, 63, 0, 64, 65, 130, 2, 0], None, 2, 1, 64, 128, True, "usual"),
     ([5], None, 1, 1, 32, 32, False, "usual"),
     ([100, 28, 300], None, 3, 3, 128, 128, True, "zeros"),
