@@ -36,7 +36,7 @@ struct GradArgs {
 template <class T, int DK, int DV, int NCW, int NLW>
 __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_reverse_kernel(const GradArgs<T> ga)
 {
-    using Sh = ChunkLds<T, DK, true, 4>;
+    using Sh = ChunkLds<T, DK, true, 4, 16 * NCW>;
     constexpr int P = Sh::P, KS = Sh::KSTEPS, KT = Sh::KT;
     const ChunkArgs<T>& a = ga.c;
     constexpr int REC = gdr_rec_bytes<T, true>();
@@ -68,17 +68,19 @@ __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_reverse_kernel(const Gra
             const size_t at = ((size_t)(t0 + c * GC) * a.Hk + hk) * DK;
             ld.load(a.k + at, a.q + at, (unsigned)(a.Hk * DK * sizeof(T)), tid,
                     min(GC, t1 - t0 - c * GC), rec0 + (size_t)c * rstep);
+            ld.load_v((ga.dO ? ga.dO : a.v) + ((size_t)(t0 + c * GC) * a.H + h) * DV + tile * NCW * 16,
+                      (unsigned)(a.H * DV * sizeof(T)), tid, min(GC, t1 - t0 - c * GC));
         };
         if (nch > 0) {
             load(0);
-            ld.store(lds, tid);
+            ld.store(lds, tid, ga.dO != nullptr);
         }
         if (nch > 1) load(1);
         __syncthreads();
         for (int i = 0; i < nch; ++i) {
             if (Sh::NBUF == 1) __syncthreads();  // the chunk's last reads
             if (i + 1 < nch) {
-                ld.store(lds + (i + 1) % Sh::NBUF * Sh::BYTES, tid);
+                ld.store(lds + (i + 1) % Sh::NBUF * Sh::BYTES, tid, ga.dO != nullptr);
                 if (i + 2 < nch) load(i + 2);
             }
             __syncthreads();
@@ -88,12 +90,11 @@ __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_reverse_kernel(const Gra
 
     const int ctile = tile * NCW + wave, col = ctile * 16 + li;
     const size_t sbase = ((size_t)n * a.H + h) * DK * DV + (size_t)(4 * gq) * DV + col;
-    const unsigned vstep = (unsigned)(a.H * DV * sizeof(T)), vcol = (unsigned)((h * DV + col) * sizeof(T));
-    auto vrow = [&](auto* p, int c) { return p + (size_t)(t0 + c * GC) * a.H * DV; };
-    unsigned off[16];
-    typename Raw1<T>::type on[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) on[i] = 0;
+    const unsigned vstep = (unsigned)(a.H * DV * sizeof(T));
+    auto value_at = [&](const char* buf, int b, int r) {
+        return to_f32(*reinterpret_cast<const T*>(buf + Sh::O_V + (16 * b + 4 * gq + r) * Sh::V_ROW +
+                                                  (wave * 16 + li) * (int)sizeof(T)));
+    };
     floatx4 dS[KT];  // scaled by sS
     ColScale sS = {1.f, 1.f}, sU = {1.f, 1.f};
     const LaneOffsets lo(lane);
@@ -106,13 +107,12 @@ __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_reverse_kernel(const Gra
                 dS[k][r] = ga.dS_T ? ga.dS_T[sbase + (size_t)(16 * k + r) * DV] : 0.f;
             m = max_abs4(m, dS[k]);
         }
-        // the first chunk is the only one that may be ragged
-        tile_offsets(vstep, vcol, gq, nch > 0 ? min(GC, t1 - t0 - (nch - 1) * GC) : GC, off);
-        if (nch > 0 && ga.dO) load_tile(vrow(ga.dO, nch - 1), off, on);
         m = column_max(m);
+        __syncthreads();  // the first chunk is in LDS
         float mv = m;
+        if (nch > 0)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) mv = fmaxf(mv, fabsf(Raw1<T>::f32(on[i])));
+            for (int i = 0; i < 16; ++i) mv = fmaxf(mv, fabsf(value_at(lds, i >> 2, i & 3)));
         mv = column_max(mv);
         if (mv > 0.f && mv < INFINITY) sU.renew(mv);
         sS = sU;
@@ -120,7 +120,6 @@ __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_reverse_kernel(const Gra
 #pragma unroll
         for (int k = 0; k < KT; ++k) dS[k] = scaled(dS[k], sS.s);
     }
-    __syncthreads();
     for (int i = 0; i < nch; ++i) {
         const int c = nch - 1 - i;
         const char* buf = lds + i % Sh::NBUF * Sh::BYTES;
@@ -132,7 +131,7 @@ __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_reverse_kernel(const Gra
 #pragma unroll
         for (int b = 0; b < 4; ++b)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) V[b][r] = Raw1<T>::f32(on[4 * b + r]);
+            for (int r = 0; r < 4; ++r) V[b][r] = value_at(buf, b, r);
         float m = 0.f;
 #pragma unroll
         for (int k = 0; k < KT; ++k) m = max_abs4(m, dS[k]);
@@ -144,8 +143,8 @@ __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_reverse_kernel(const Gra
         }
         Split sp[KS], s1[2], s2[2];
         floatx4 y[4];
-        T out[16];
-        half8 kc[KT][2];
+        float out[16];
+        floatx4 z1[4], z2[4];
         float mu;
         for (int tries = 0;; ++tries) {  // as in gdr_walk
             half8 kf[KS][4], ah[TRI], al[TRI];
@@ -240,10 +239,6 @@ __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_reverse_kernel(const Gra
             request_fence();
             // Y = D - W^T (beta D)
 #pragma unroll
-            for (int k = 0; k < KT; ++k)
-#pragma unroll
-                for (int s = 0; s < 2; ++s) kc[k][s] = frag_cols<KS>(buf + Sh::O_K, lo, k, s);
-#pragma unroll
             for (int b = 0; b < 4; ++b) d[b] = zero4();
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
@@ -255,7 +250,6 @@ __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_reverse_kernel(const Gra
                 for (int b = 0; b < 2 * s + 2; ++b) d[b] = mma(wl[tri_frag_t(b, s)], ds[s].hi, d[b]);
             }
             request_fence();
-            floatx4 z1[4], z2[4];
             float mz = 0.f;
             mu = mg;
 #pragma unroll
@@ -264,17 +258,12 @@ __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_reverse_kernel(const Gra
                 for (int r = 0; r < 4; ++r) {
                     y[b][r] = fmaf(-wr[b][r], d[b][r], D[b][r]);
                     const float dv = be[b][r] * y[b][r];
-                    out[4 * b + r] = from_f32<T>(dv * sU.i);
+                    out[4 * b + r] = dv * sU.i;
                     z1[b][r] = (-g1[b][r] * zs) * dv;
                     z2[b][r] = (g2[b][r] * zs) * G[b][r];
                 }
                 mu = max_abs4(mu, y[b]);
                 mz = max_abs4(max_abs4(mz, z1[b]), z2[b]);
-            }
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                s1[s] = split(z1[2 * s], z1[2 * s + 1]);
-                s2[s] = split(z2[2 * s], z2[2 * s + 1]);
             }
             if (!__any(too_large(mb) || too_large(mu) || too_large(mz)) || tries == 8) break;
             mg = column_max(mg);
@@ -293,15 +282,21 @@ __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_reverse_kernel(const Gra
 #pragma unroll
             for (int k = 0; k < KT; ++k) dS[k] = scaled(dS[k], f);
         }
-        half8 qc[KT][2];
+        half8 kc[KT][2], qc[KT][2];
 #pragma unroll
         for (int k = 0; k < KT; ++k)
 #pragma unroll
-            for (int s = 0; s < 2; ++s) qc[k][s] = frag_cols<KS>(buf + Sh::O_Q, lo, k, s);
+            for (int s = 0; s < 2; ++s) {
+                kc[k][s] = frag_cols<KS>(buf + Sh::O_K, lo, k, s);
+                qc[k][s] = frag_cols<KS>(buf + Sh::O_Q, lo, k, s);
+            }
         request_fence();
-        store_tile(vrow(ga.dv, c), off, gq, len, out);
-        if (i == 0) tile_offsets(vstep, vcol, gq, GC, off);
-        if (c > 0 && ga.dO) load_tile(vrow(ga.dO, c - 1), off, on);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            s1[s] = split(z1[2 * s], z1[2 * s + 1]);
+            s2[s] = split(z2[2 * s], z2[2 * s + 1]);
+        }
+        store_tile(ga.dv + ((size_t)(t0 + c * GC) * a.H + h) * DV + ctile * 16, vstep, lane, len, out);
         {
             const size_t kept = (size_t)(g0 + c) * a.H + h;
             _Float16* ks = ga.keep.dS + kept * keep_state<T, DK>(DV) + (size_t)(ctile * KS * 64 + lane) * 8;
@@ -402,7 +397,7 @@ __device__ __forceinline__ float before16(float x)
 
 template <class T, int DK, int DV>
 struct GradLds {
-    using Sh = ChunkLds<T, DK, true, -1>;
+    using Sh = ChunkLds<T, DK, true, -1, 0>;
     static constexpr int P = Sh::P;
     static constexpr int ROWS = (int)keep_rows<T>(DV) * 2;        // bytes of E or Y
     static constexpr int STATE = (int)keep_state<T, DK>(DV) * 2;  // of S or dS

@@ -281,8 +281,9 @@ __device__ __forceinline__ half8 frag_cols(const char* m, const LaneOffsets& lo,
     return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// LDS of one chunk: K, Q (P parts each, Q if wanted), then the record's head and MATS of its matrices.
-template <class T, int DK, bool Q, int MATS>
+// LDS of one chunk: K, Q (P parts each, Q if wanted), the record's head and MATS of its matrices, and VC
+// columns of V or dO as stored ([64][V_ROW bytes]; bf16: 16 more than a row, for the banks).
+template <class T, int DK, bool Q, int MATS, int VC>
 struct ChunkLds {
     static constexpr int P = gdr_parts<T>();
     static constexpr int KSTEPS = DK < 32 ? 1 : DK / 32;
@@ -290,7 +291,9 @@ struct ChunkLds {
     static constexpr int RB = 4 * KSTEPS * 1024;  // one part of K or Q
     static constexpr int O_K = 0, O_Q = P * RB, O_REC = O_Q + (Q ? P * RB : 0);
     static constexpr int REC = MATS < 0 ? 0 : REC_HEAD + MATS * TRI_BYTES;
-    static constexpr int BYTES = O_REC + REC;
+    static constexpr int O_V = O_REC + REC, V_ROW = VC * (int)sizeof(T) + (VC > 0 && P == 1 ? 16 : 0);
+    static constexpr int VCOLS = VC;
+    static constexpr int BYTES = O_V + GC * V_ROW;
     static constexpr int NBUF = 2 * BYTES <= 160 * 1024 ? 2 : 1;
     static constexpr bool q = Q;
 };
@@ -351,6 +354,22 @@ struct Loader {
     Raw8<T> k[TPT], q[Lds::q ? TPT : 1];
     float4 ks[TPT], qs[Lds::q ? TPT : 1];  // the rows' scales
     uint4 rec[RECP > 0 ? RECP : 1];
+    static constexpr int VPR = Lds::VCOLS > 0 ? Lds::VCOLS * (int)sizeof(T) / 16 : 1;  // pieces of a row
+    static constexpr int VP = Lds::VCOLS > 0 ? (GC * VPR + NT - 1) / NT : 0;          // of V
+    uint4 v[VP > 0 ? VP : 1];
+
+    // The columns at p of V or dO, vstep bytes from token to token. (What is to count as 0 is loaded
+    // from elsewhere and dropped at the store: a load in a branch would be waited for behind it.)
+    __device__ __forceinline__ void load_v(const T* p, unsigned vstep, int tid, int len)
+    {
+#pragma unroll
+        for (int j = 0; j < VP; ++j) {
+            const int i = (tid + NT * j) % (GC * VPR);
+            v[j] = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(p) +
+                                                   (unsigned)min(i / VPR, len - 1) * vstep +
+                                                   16 * (i % VPR));
+        }
+    }
 
     // step: bytes of a token's row over all key heads
     __device__ __forceinline__ void load(const T* kbase, const T* qbase, unsigned step, int tid,
@@ -382,7 +401,7 @@ struct Loader {
         }
     }
 
-    __device__ __forceinline__ void store(char* buf, int tid)
+    __device__ __forceinline__ void store(char* buf, int tid, bool keep_v = true)
     {
 #pragma unroll
         for (int j = 0; j < TPT; ++j) {
@@ -393,45 +412,61 @@ struct Loader {
 #pragma unroll
         for (int j = 0; j < RECP; ++j)
             reinterpret_cast<uint4*>(buf + Lds::O_REC)[min(tid + NT * j, Lds::REC / 16 - 1)] = rec[j];
+#pragma unroll
+        for (int j = 0; j < VP; ++j) {
+            const int i = (tid + NT * j) % (GC * VPR);
+            *reinterpret_cast<uint4*>(buf + Lds::O_V + i / VPR * Lds::V_ROW + 16 * (i % VPR)) =
+                keep_v ? v[j] : make_uint4(0, 0, 0, 0);
+        }
     }
 };
 
-// Byte offsets of a lane's 16 places of a chunk's column (result tile layout) from the chunk's first
-// token: rows past the end repeat the last one. step: bytes of a token's row, at: of this lane's column.
-__device__ __forceinline__ void tile_offsets(unsigned step, unsigned at, int gq, int len, unsigned* off)
+// Stores a lane's 16 values of a column of [tokens][H][DV] (result tile layout: rows 16b + 4g + r of
+// column i), step bytes from token to token, of a chunk of len tokens. Four lanes of adjacent columns
+// exchange their four rows (a transpose within each quad), so that each stores four adjacent columns of
+// one row: 4 stores of 8 (float32: 16) bytes in place of 16 of 2 (4). base: the chunk's first token at the
+// wave's first column.
+template <int S>
+__device__ __forceinline__ unsigned quad_lane(unsigned x)  // of lane S of this lane's quad
 {
-#pragma unroll
-    for (int b = 0; b < 4; ++b)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-            off[4 * b + r] = (unsigned)min(16 * b + 4 * gq + r, len - 1) * step + at;
+    return (unsigned)__builtin_amdgcn_mov_dpp((int)x, S * 0x55, 0xf, 0xf, true);
 }
-// Values kept as loaded, a register each (a bf16 zero-extended): packed two to a register, they would be
-// waited for at once.
 template <class T>
-__device__ __forceinline__ void load_tile(const T* p, const unsigned* off, typename Raw1<T>::type* x)
+__device__ __forceinline__ void store_tile(T* base, unsigned step, int lane, int len, const float* x)
 {
+    const int gq = lane >> 4, li = lane & 15, j = li & 3;
+    char* p = reinterpret_cast<char*>(base) + (unsigned)(4 * gq + j) * step + (li & ~3) * sizeof(T);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const char* at = reinterpret_cast<const char*>(p) + off[i];
-        if constexpr (sizeof(T) == 2)
-            x[i] = *reinterpret_cast<const unsigned short*>(at);
-        else
-            x[i] = *reinterpret_cast<const float*>(at);
-    }
-}
-// Stores of a chunk of len tokens: whole chunks without a branch per row.
-template <class T>
-__device__ __forceinline__ void store_tile(T* p, const unsigned* off, int gq, int len, const T* x)
-{
-    if (len == GC) {
+    for (int b = 0; b < 4; ++b) {
+        const bool in = 16 * b + 4 * gq + j < len;
+        char* at = p + (size_t)(16 * b) * step;
+        if constexpr (sizeof(T) == 2) {
+            const bf16x4 y = {(bf16)x[4 * b], (bf16)x[4 * b + 1], (bf16)x[4 * b + 2], (bf16)x[4 * b + 3]};
+            const uint2 z = __builtin_bit_cast(uint2, y);  // rows 0 and 1, 2 and 3
+            // this lane's row of the quad's lanes: the pair by j / 2, its half by j % 2
+            const unsigned half = j & 1 ? 0x07060302u : 0x05040100u;
+            const unsigned x0 = quad_lane<0>(z.x), y0 = quad_lane<0>(z.y);
+            const unsigned x1 = quad_lane<1>(z.x), y1 = quad_lane<1>(z.y);
+            const unsigned x2 = quad_lane<2>(z.x), y2 = quad_lane<2>(z.y);
+            const unsigned x3 = quad_lane<3>(z.x), y3 = quad_lane<3>(z.y);
+            const unsigned v0 = j < 2 ? x0 : y0, v1 = j < 2 ? x1 : y1;
+            const unsigned v2 = j < 2 ? x2 : y2, v3 = j < 2 ? x3 : y3;
+            const uint2 out = make_uint2(__builtin_amdgcn_perm(v1, v0, half),
+                                         __builtin_amdgcn_perm(v3, v2, half));
+            if (in) *reinterpret_cast<uint2*>(at) = out;
+        } else {
+            unsigned z[4], v[4];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) *reinterpret_cast<T*>(reinterpret_cast<char*>(p) + off[i]) = x[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-            if (16 * (i >> 2) + 4 * gq + (i & 3) < len)
-                *reinterpret_cast<T*>(reinterpret_cast<char*>(p) + off[i]) = x[i];
+            for (int r = 0; r < 4; ++r) z[r] = __float_as_uint(x[4 * b + r]);
+            auto mine = [&](unsigned a, unsigned b, unsigned c, unsigned d) {
+                return j < 2 ? (j == 0 ? a : b) : (j == 2 ? c : d);
+            };
+            v[0] = mine(quad_lane<0>(z[0]), quad_lane<0>(z[1]), quad_lane<0>(z[2]), quad_lane<0>(z[3]));
+            v[1] = mine(quad_lane<1>(z[0]), quad_lane<1>(z[1]), quad_lane<1>(z[2]), quad_lane<1>(z[3]));
+            v[2] = mine(quad_lane<2>(z[0]), quad_lane<2>(z[1]), quad_lane<2>(z[2]), quad_lane<2>(z[3]));
+            v[3] = mine(quad_lane<3>(z[0]), quad_lane<3>(z[1]), quad_lane<3>(z[2]), quad_lane<3>(z[3]));
+            if (in) *reinterpret_cast<uint4*>(at) = make_uint4(v[0], v[1], v[2], v[3]);
+        }
     }
 }
 

@@ -74,14 +74,14 @@ __device__ __forceinline__ floatx4 scaled(const floatx4& x, float f)
 
 __device__ __forceinline__ void st8(_Float16* p, half8 x) { *reinterpret_cast<half8*>(p) = x; }
 
-template <class T, int DK, bool BWD>
-using WalkLds = ChunkLds<T, DK, !BWD, BWD ? 2 : 2 + gdr_parts<T>()>;
+template <class T, int DK, int NCW, bool BWD>
+using WalkLds = ChunkLds<T, DK, !BWD, BWD ? 2 : 2 + gdr_parts<T>(), 16 * NCW>;
 
 template <class T, int DK, int DV, int NCW, int NLW, bool BWD>
 __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_walk_kernel(const ChunkArgs<T> a,
                                                                     const GdrKeep keep)
 {
-    using Sh = WalkLds<T, DK, BWD>;
+    using Sh = WalkLds<T, DK, NCW, BWD>;
     constexpr int P = Sh::P, KS = Sh::KSTEPS, KT = Sh::KT;
     constexpr int REC = gdr_rec_bytes<T, BWD>();
     constexpr int TILES = DV / (16 * NCW);  // workgroups of a chain
@@ -112,6 +112,8 @@ __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_walk_kernel(const ChunkA
             const size_t at = ((size_t)(t0 + c * GC) * a.Hk + hk) * DK;
             ld.load(a.k + at, a.q + at, (unsigned)(a.Hk * DK * sizeof(T)), tid,
                     min(GC, t1 - t0 - c * GC), rec0 + (size_t)c * rstep);
+            ld.load_v(a.v + ((size_t)(t0 + c * GC) * a.H + h) * DV + tile * NCW * 16,
+                      (unsigned)(a.H * DV * sizeof(T)), tid, min(GC, t1 - t0 - c * GC));
         };
         if (nch > 0) {
             load(0);
@@ -132,14 +134,10 @@ __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_walk_kernel(const ChunkA
 
     const int ctile = tile * NCW + wave, col = ctile * 16 + li;
     const size_t sbase = ((size_t)n * a.H + h) * DK * DV + (size_t)(4 * gq) * DV + col;
-    const unsigned vstep = (unsigned)(a.H * DV * sizeof(T)), vcol = (unsigned)((h * DV + col) * sizeof(T));
-    auto vrow = [&](auto* p, int c) { return p + (size_t)(t0 + c * GC) * a.H * DV; };
-    unsigned off[16];
-    typename Raw1<T>::type vn[16];
-    auto load_v = [&](int c) {
-        const int len = t1 - t0 - c * GC;
-        if (len < GC) tile_offsets(vstep, vcol, gq, len, off);  // the last chunk
-        load_tile(vrow(a.v, c), off, vn);
+    const unsigned vstep = (unsigned)(a.H * DV * sizeof(T));
+    auto value_at = [&](const char* buf, int b, int r) {
+        return to_f32(*reinterpret_cast<const T*>(buf + Sh::O_V + (16 * b + 4 * gq + r) * Sh::V_ROW +
+                                                  (wave * 16 + li) * (int)sizeof(T)));
     };
     floatx4 S[KT];  // scaled by sS
     ColScale sS = {1.f, 1.f}, sU = {1.f, 1.f};
@@ -153,13 +151,12 @@ __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_walk_kernel(const ChunkA
                 S[k][r] = a.S0 ? a.S0[sbase + (size_t)(16 * k + r) * DV] : 0.f;
             m = max_abs4(m, S[k]);
         }
-        tile_offsets(vstep, vcol, gq, GC, off);
-        if (nch > 0) load_v(0);
         m = column_max(m);
+        __syncthreads();  // the first chunk is in LDS
         float mv = m;
         if (nch > 0)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) mv = fmaxf(mv, fabsf(Raw1<T>::f32(vn[i])));
+            for (int i = 0; i < 16; ++i) mv = fmaxf(mv, fabsf(value_at(lds, i >> 2, i & 3)));
         mv = column_max(mv);
         if (mv > 0.f && mv < INFINITY) sU.renew(mv);
         sS = sU;
@@ -167,19 +164,35 @@ __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_walk_kernel(const ChunkA
 #pragma unroll
         for (int k = 0; k < KT; ++k) S[k] = scaled(S[k], sS.s);
     }
-    __syncthreads();
+    Split ys[2] = {};
+    half8 kc[KT][2] = {};
+    float gc = 1.f;
+    // S <- 2^l_C S + K^T (2^(l_C - l) U) of the chunk before, whose operands are in registers: it runs
+    // behind that chunk's barrier, while the next one's operands are on their way
+    auto advance = [&]() {
+#pragma unroll
+        for (int k = 0; k < KT; ++k) S[k] = scaled(S[k], gc);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+#pragma unroll
+            for (int k = 0; k < KT; ++k) S[k] = mma(kc[k][s], ys[s].hi, S[k]);
+#pragma unroll
+            for (int k = 0; k < KT; ++k) S[k] = mma(kc[k][s], ys[s].lo, S[k]);
+        }
+    };
     for (int c = 0; c < nch; ++c) {
         const char* buf = lds + c % Sh::NBUF * Sh::BYTES;
         const float* fac = reinterpret_cast<const float*>(buf + Sh::O_REC);
         const char* tri = buf + Sh::O_REC + REC_HEAD;
         const int len = min(GC, t1 - t0 - c * GC);
         auto factor = [&](int f, int b, float* x) { unpack4(ld4(fac + f * GC + 16 * b + 4 * gq), x); };
-        floatx4 V[4];
+        half8 kf[KS][4];
 #pragma unroll
-        for (int b = 0; b < 4; ++b)
+        for (int s = 0; s < KS; ++s)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) V[b][r] = Raw1<T>::f32(vn[4 * b + r]);
-
+            for (int b = 0; b < 4; ++b) kf[s][b] = frag_rows<KS>(buf + Sh::O_K, lo, b, s);
+        request_fence();
+        if (P == 1) advance();
         float m = 0.f;
 #pragma unroll
         for (int k = 0; k < KT; ++k) m = max_abs4(m, S[k]);
@@ -189,20 +202,13 @@ __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_walk_kernel(const ChunkA
 #pragma unroll
             for (int k = 0; k < KT; ++k) S[k] = scaled(S[k], f);
         }
-        Split sp[KS], ys[2], us[2];
-        floatx4 o[4], e[4];
-        half8 kc[KT][2];
+        Split sp[KS];
+        floatx4 o[4], e[4], u[4], y[4];
         float mu;
         // Again with other scales where a column has left f16's range, which costs a chunk's time and
         // hardly happens: the scales follow the columns. Ends at the latest when a scale cannot fall.
         for (int tries = 0;; ++tries) {
-            half8 kf[KS][4];
             float g1[4][4], be[4][4];
-#pragma unroll
-            for (int s = 0; s < KS; ++s)
-#pragma unroll
-                for (int b = 0; b < 4; ++b) kf[s][b] = frag_rows<KS>(buf + Sh::O_K, lo, b, s);
-            request_fence();
 #pragma unroll
             for (int s = 0; s < KS; ++s) sp[s] = split(S[2 * s], KT > 1 ? S[2 * s + 1] : zero4());
             request_fence();
@@ -234,6 +240,11 @@ __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_walk_kernel(const ChunkA
             }
             request_fence();
             half8 wh[TRI], wl[TRI];
+            float V[4][4];
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) V[b][r] = value_at(buf, b, r);
 #pragma unroll
             for (int i = 0; i < TRI; ++i) {
                 wh[i] = frag_ld(tri, i, lane);
@@ -272,10 +283,6 @@ __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_walk_kernel(const ChunkA
                 factor(F_WR, b, wr[b]);
                 factor(F_W, b, w[b]);
             }
-#pragma unroll
-            for (int k = 0; k < KT; ++k)
-#pragma unroll
-                for (int s = 0; s < 2; ++s) kc[k][s] = frag_cols<KS>(buf + Sh::O_K, lo, k, s);
             floatx4 d[4];
 #pragma unroll
             for (int b = 0; b < 4; ++b) d[b] = zero4();
@@ -289,7 +296,6 @@ __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_walk_kernel(const ChunkA
                 for (int b = 2 * s; b < 4; ++b) d[b] = mma(wl[tri_frag(b, s)], bs[s].hi, d[b]);
             }
             request_fence();
-            floatx4 u[4], y[4];
             const float yscale = sS.s * sU.i;
             float my = 0.f;
             mu = 0.f;
@@ -305,12 +311,6 @@ __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_walk_kernel(const ChunkA
                 if (BWD) mu = max_abs4(mu, u[b]);
                 my = max_abs4(my, y[b]);
             }
-            ys[0] = split(y[0], y[1]);
-            ys[1] = split(y[2], y[3]);
-            if (!BWD) {
-                us[0] = split(u[0], u[1]);
-                us[1] = split(u[2], u[3]);
-            }
             if (!__any(too_large(mb) || too_large(mu) || too_large(my)) || tries == 8) break;
             mb = column_max(mb);
             mu = column_max(mu);
@@ -325,7 +325,25 @@ __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_walk_kernel(const ChunkA
 #pragma unroll
             for (int k = 0; k < KT; ++k) S[k] = scaled(S[k], f);
         }
-        if (c + 1 < nch && t1 - t0 - (c + 1) * GC >= GC) load_tile(vrow(a.v, c + 1), off, vn);
+#pragma unroll
+        for (int k = 0; k < KT; ++k)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) kc[k][s] = frag_cols<KS>(buf + Sh::O_K, lo, k, s);
+        half8 af[TRI];
+        float gv[4][4], av[4][4];
+        if (!BWD) {
+#pragma unroll
+            for (int i = 0; i < TRI; ++i) af[i] = frag_ld(tri, 2 * TRI + i, lane);
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                factor(F_GQ, b, gv[b]);
+                factor(F_AR, b, av[b]);
+            }
+        }
+        gc = fac[REC_FACTORS];
+        request_fence();
+        ys[0] = split(y[0], y[1]);
+        ys[1] = split(y[2], y[3]);
         if (BWD) {
             const size_t kept = (size_t)(g0 + c) * a.H + h;
             _Float16* ks = keep.S + kept * keep_state<T, DK>(DV) + (size_t)(ctile * KS * 64 + lane) * 8;
@@ -347,35 +365,25 @@ __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_walk_kernel(const ChunkA
                 sc[KEEP_E * DV] = sU.i;
             }
         }
-        // S <- 2^l_C S + K^T (2^(l_C - l) U)
-        const float gc = fac[REC_FACTORS];
-        half8 af[TRI];
-        float gv[4][4], av[4][4];
-        if (!BWD) {
+        if (P == 2) {  // with the low halves of K, from LDS
+            advance();
 #pragma unroll
-            for (int i = 0; i < TRI; ++i) af[i] = frag_ld(tri, 2 * TRI + i, lane);
-#pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                factor(F_GQ, b, gv[b]);
-                factor(F_AR, b, av[b]);
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < KT; ++k) S[k] = scaled(S[k], gc);
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-#pragma unroll
-            for (int k = 0; k < KT; ++k) S[k] = mma(kc[k][s], ys[s].hi, S[k]);
-#pragma unroll
-            for (int k = 0; k < KT; ++k) S[k] = mma(kc[k][s], ys[s].lo, S[k]);
-            if (P == 2)
+            for (int s = 0; s < 2; ++s)
 #pragma unroll
                 for (int k = 0; k < KT; ++k)
                     S[k] = mma(frag_cols<KS>(buf + Sh::O_K + Sh::RB, lo, k, s), ys[s].hi, S[k]);
         }
         if (!BWD) {  // O = scale (2^l Q S + A U)
             floatx4 d[4];
-            T out[16];
+            float out[16];
+            Split us[2];
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                if (P == 2)
+                    us[s] = split(u[2 * s], u[2 * s + 1]);
+                else
+                    us[s].hi = to_half(u[2 * s], u[2 * s + 1]);
+            }
 #pragma unroll
             for (int b = 0; b < 4; ++b) d[b] = zero4();
 #pragma unroll
@@ -392,17 +400,17 @@ __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_walk_kernel(const ChunkA
             for (int b = 0; b < 4; ++b)
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    out[4 * b + r] = from_f32<T>(
-                        fmaf(gv[b][r], o[b][r] * sS.i, av[b][r] * (d[b][r] * sU.i)));
-            store_tile(vrow(a.o, c), off, gq, len, out);
+                    out[4 * b + r] =
+                        fmaf(gv[b][r], o[b][r] * sS.i, av[b][r] * (d[b][r] * sU.i));
+            store_tile(a.o + ((size_t)(t0 + c * GC) * a.H + h) * DV + ctile * 16, vstep, lane, len, out);
         }
-        if (c + 1 < nch && t1 - t0 - (c + 1) * GC < GC) load_v(c + 1);  // the last chunk, not whole
         // a column of writes that has become small gets its bits back
         mu = column_max(mu);
         if (mu < 4.f && mu > 0.f) sU.renew(mu);
         if (Sh::NBUF == 1) __syncthreads();
         __syncthreads();
     }
+    if (P == 1) advance();
     if (a.S_T)
 #pragma unroll
         for (int k = 0; k < KT; ++k)
