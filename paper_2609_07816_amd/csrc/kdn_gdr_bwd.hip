@@ -352,11 +352,12 @@ __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_reverse_kernel(const Gra
 }
 
 // ------------------------------------------------------------------------------------------
-// gdr_grad: a workgroup of eight waves per (chunk, key head); wave (w, half) has tokens 16w .. 16w+15
-// and, of the products with the state, half of the key channels; the value heads of the key head one
-// after another, dQ and dK summed in registers in that order. E and Y, then S and dS come through LDS,
-// from where the transposing read gives either side's fragments; the scales of the value columns, over
-// which the products contract, are folded into the A side (each over the largest).
+// gdr_grad: a workgroup of four waves per (chunk, key head), wave w has tokens 16w .. 16w+15; the value
+// heads of the key head one after another, dQ and dK summed in registers in that order. E and Y, then C
+// and Z, then S, then dS come through one region of LDS (70 KB in all at d 128 in bf16: two workgroups on
+// a CU, whose waits overlap), from where the transposing read gives either side's fragments; the scales
+// of the value columns, over which the products contract, are folded into the A side (each over the
+// largest).
 // ------------------------------------------------------------------------------------------
 template <int P, int N>
 struct Operand {
@@ -401,41 +402,42 @@ struct GradLds {
     static constexpr int P = Sh::P;
     static constexpr int ROWS = (int)keep_rows<T>(DV) * 2;        // bytes of E or Y
     static constexpr int STATE = (int)keep_state<T, DK>(DV) * 2;  // of S or dS
-    static constexpr bool BOTH = P == 1;                          // S and dS at once
-    static constexpr int R = 2 * ROWS > (BOTH ? 2 : 1) * STATE ? 2 * ROWS : (BOTH ? 2 : 1) * STATE;
+    static constexpr int MATRIX = 64 * 68 * 4;                    // C and Z
+    static constexpr int R0 = 2 * ROWS > STATE ? 2 * ROWS : STATE;
+    // float32 calls, which are alone on their CU as it is, keep C and Z in a place of their own and so
+    // out of the registers
+    static constexpr bool SHARE = P == 1;
+    static constexpr int R = !SHARE ? R0 + MATRIX : R0 > MATRIX ? R0 : MATRIX;
 };
 
 constexpr int CP = 68;  // floats of a row of the 64 x 64 matrix in LDS
 
 template <class T, int DK, int DV>
-__global__ __launch_bounds__(512) void gdr_grad_kernel(const GradArgs<T> ga)
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void gdr_grad_kernel(const GradArgs<T> ga)
 {
     using Ls = GradLds<T, DK, DV>;
     using Sh = typename Ls::Sh;
-    constexpr int P = Sh::P, KS = Sh::KSTEPS, KT = Sh::KT, NT = 512;
+    constexpr int P = Sh::P, KS = Sh::KSTEPS, KT = Sh::KT, NT = 256;
     constexpr int REC = gdr_rec_bytes<T, true>();
-    constexpr int VS = DV < 32 ? 1 : DV / 32, VT = DV / 16, KH = (KT + 1) / 2;
+    constexpr int VS = DV < 32 ? 1 : DV / 32, VT = DV / 16;
     constexpr int DVP = VS * 32;
     const ChunkArgs<T>& a = ga.c;
     __shared__ __align__(16) char lds[Sh::BYTES];     // K, Q
-    __shared__ __align__(16) char reg[Ls::R];         // E and Y, then S and dS
-    __shared__ __align__(16) float sC[GC * CP];       // C on and below the diagonal, Z^T above it
+    __shared__ __align__(16) char reg[Ls::R];         // E and Y; C and Z; S; dS
+    float* sC = reinterpret_cast<float*>(reg + (Ls::SHARE ? 0 : Ls::R0));        // C on and below the diagonal, Z^T above it
     __shared__ __align__(16) _Float16 s_fold[FOLD_COUNT][DVP];
     __shared__ float s_top[FOLD_COUNT], s_inv[KEEP_COUNT][DV];
     __shared__ double s_l[GC];
-    __shared__ float s_be[GC], s_ri[GC], s_ks[GC], s_qs[GC], s_dot[8];
-    __shared__ float s_reads[2][GC], s_writes[2][GC], s_cross[4][GC], s_tot[GC];
+    __shared__ float s_be[GC], s_ri[GC], s_ks[GC], s_qs[GC], s_dot[4];
+    __shared__ float s_reads[GC], s_writes[GC], s_cross[4][GC];
     __shared__ float s_ic[GC], s_it[GC], s_iz[GC];  // inverse scales of the rows of C, C^T, Z + Z^T
     const int g = blockIdx.x / a.Hk, hk = blockIdx.x % a.Hk;
     int n, c0, c1;
     if (!gdr_locate(a.seq, g, n, c0, c1)) return;
-    const int len = c1 - c0, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, gq = lane >> 4,
-              li = lane & 15, w = wave & 3, half = wave >> 2, row = 16 * w + li;
-    const LaneOffsets lo(lane);
-    const int tr = lo.tr[0];
+    const int len = c1 - c0, thread = threadIdx.x;
 
     if (DK == 16) {  // the upper half of the 32 contracted places stays 0
-        for (int i = tid; i < Sh::BYTES / 16; i += NT)
+        for (int i = thread; i < Sh::BYTES / 16; i += NT)
             reinterpret_cast<uint4*>(lds)[i] = make_uint4(0, 0, 0, 0);
         __syncthreads();
     }
@@ -443,37 +445,51 @@ __global__ __launch_bounds__(512) void gdr_grad_kernel(const GradArgs<T> ga)
     {
         Loader<T, DK, Sh, NT, 0> ld;
         const size_t at = ((size_t)c0 * a.Hk + hk) * DK;
-        ld.load(a.k + at, a.q + at, (unsigned)(a.Hk * DK * sizeof(T)), tid, len, rec);
-        ld.store(lds, tid);
+        ld.load(a.k + at, a.q + at, (unsigned)(a.Hk * DK * sizeof(T)), thread, len, rec);
+        ld.store(lds, thread);
         const float* fac = reinterpret_cast<const float*>(rec);
-        if (tid < GC) {  // 0 for the tokens past the end, as the rows' scales
-            s_ks[tid] = fac[F_KS * GC + tid] > 0.f ? pow2_inverse(fac[F_KS * GC + tid]) : 0.f;
-            s_qs[tid] = fac[F_QS * GC + tid] > 0.f ? pow2_inverse(fac[F_QS * GC + tid]) : 0.f;
+        if (thread < GC) {  // 0 for the tokens past the end, as the rows' scales
+            s_ks[thread] = fac[F_KS * GC + thread] > 0.f ? pow2_inverse(fac[F_KS * GC + thread]) : 0.f;
+            s_qs[thread] = fac[F_QS * GC + thread] > 0.f ? pow2_inverse(fac[F_QS * GC + thread]) : 0.f;
         }
     }
-    floatx4 dq[KH], dk[KH];
+    floatx4 dq[KT], dk[KT];
 #pragma unroll
-    for (int k = 0; k < KH; ++k) dq[k] = dk[k] = zero4();
-
-    // fragments of E or Y: tokens 16b .. as rows, value columns 32s ..
-    auto rows_frag = [&](const char* x, int b, int s) {
-        const char* p = x + (b >> 1) * 1024 + (b & 1) * 8 + tr;
-        const half4 y = lds_read_tr(p + 2 * s * 2048);
-        const half4 z = VT > 1 ? lds_read_tr(p + (2 * s + 1) * 2048) : half4{0, 0, 0, 0};
-        return __builtin_shufflevector(y, z, 0, 1, 2, 3, 4, 5, 6, 7);
-    };
-    // of S or dS: key channels 16k .. as rows, value columns 32s ..
-    auto state_frag = [&](const char* x, int k, int s) {
-        const char* p = x + (k >> 1) * 1024 + (k & 1) * 8 + tr;
-        const half4 y = lds_read_tr(p + 2 * s * KS * 1024);
-        const half4 z = VT > 1 ? lds_read_tr(p + (2 * s + 1) * KS * 1024) : half4{0, 0, 0, 0};
-        return __builtin_shufflevector(y, z, 0, 1, 2, 3, 4, 5, 6, 7);
-    };
+    for (int k = 0; k < KT; ++k) dq[k] = dk[k] = zero4();
 
 #pragma unroll 1
     for (int hv = 0; hv < a.rep; ++hv) {
         const int h = hk * a.rep + hv;
         const size_t kept = (size_t)g * a.H + h;
+        // The places in LDS and the comparisons with them are the same for every value head: what this
+        // hides is that, or all would be computed before the loop, into more registers than there are
+        // (1700 bytes a lane of scratch at d 128).
+        int tid = thread;
+        asm volatile("" : "+v"(tid));
+        const int lane = tid & 63, gq = lane >> 4, li = lane & 15, w = __builtin_amdgcn_readfirstlane(tid >> 6),
+                  row = 16 * w + li;
+        const LaneOffsets lo(lane);
+        int wrow[4], wtr[4];  // this wave's block
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int rot = (i + KS * w) & 3;
+            wrow[i] = w * KS * 1024 + gq * 256 + ((li + rot) & 15) * 16;
+            wtr[i] = w * KS * 1024 + (li & 3) * 256 + ((4 * gq + (li >> 2) + rot) & 15) * 16;
+        }
+        // fragments of E or Y: tokens 16b .. as rows, value columns 32s ..
+        auto rows_frag = [&](const char* x, int b, int s) {
+            const char* p = x + (b >> 1) * 1024 + (b & 1) * 8 + lo.tr[0];
+            const half4 y = lds_read_tr(p + 2 * s * 2048);
+            const half4 z = VT > 1 ? lds_read_tr(p + (2 * s + 1) * 2048) : half4{0, 0, 0, 0};
+            return __builtin_shufflevector(y, z, 0, 1, 2, 3, 4, 5, 6, 7);
+        };
+        // of S or dS: key channels 16k .. as rows, value columns 32s ..
+        auto state_frag = [&](const char* x, int k, int s) {
+            const char* p = x + (k >> 1) * 1024 + (k & 1) * 8 + lo.tr[0];
+            const half4 y = lds_read_tr(p + 2 * s * KS * 1024);
+            const half4 z = VT > 1 ? lds_read_tr(p + (2 * s + 1) * KS * 1024) : half4{0, 0, 0, 0};
+            return __builtin_shufflevector(y, z, 0, 1, 2, 3, 4, 5, 6, 7);
+        };
         rec = a.rec + kept * REC;
         const float* fac = reinterpret_cast<const float*>(rec);
         const uint4* gE = reinterpret_cast<const uint4*>(ga.keep.E + kept * keep_rows<T>(DV));
@@ -522,45 +538,61 @@ __global__ __launch_bounds__(512) void gdr_grad_kernel(const GradArgs<T> ga)
                     for (int e = 0; e < 8; ++e) go.lo[s][e] = (_Float16)(x[s][e] - (float)go.hi[s][e]);
                 }
             }
-            if (half == 0 && gq == 0) s_ri[row] = inv;
+            if (gq == 0) s_ri[row] = inv;
         }
         __syncthreads();
-        if (wave < FOLD_COUNT) {  // a wave per product: its columns' scales over the largest
-            constexpr int first[FOLD_COUNT] = {KEEP_E, KEEP_Y, KEEP_S, KEEP_Y, KEEP_E};
-            constexpr int second[FOLD_COUNT] = {-1, KEEP_E, -1, KEEP_S, KEEP_DS};
-            int f1 = 0, f2 = 0;
+        {  // the products' column scales over the largest: a wave each, wave 0 also the last one
+            auto fold_of = [&](int p, const float* f1, const float* f2) {
+                float x[2], top = 0x1p-120f;
 #pragma unroll
-            for (int i = 0; i < FOLD_COUNT; ++i)
-                if (wave == i) {
-                    f1 = first[i];
-                    f2 = second[i];
+                for (int j = 0; j < 2; ++j) {
+                    const int i = lane + 64 * j;
+                    x[j] = i < DV ? f1[i] * (f2 ? f2[i] : 1.f) : 0.f;
+                    top = fmaxf(top, x[j]);
                 }
-            float x[2];
-            float top = 0x1p-120f;
+                top = fminf(wave_max(top), 0x1p120f);
+                const float r = pow2_inverse(top);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int i = lane + 64 * j;
-                x[j] = i < DV ? s_inv[f1][i] * (f2 < 0 ? 1.f : s_inv[f2][i]) : 0.f;
-                top = fmaxf(top, x[j]);
+                for (int j = 0; j < 2; ++j) {
+                    const int i = lane + 64 * j;
+                    if (i < DVP) s_fold[p][col_place(i)] = (_Float16)(x[j] * r);
+                }
+                if (lane == 0) s_top[p] = top;
+            };
+            if (w == 0) {
+                fold_of(FOLD_E, s_inv[KEEP_E], nullptr);
+                fold_of(FOLD_S, s_inv[KEEP_S], nullptr);
+            } else if (w == 1) {
+                fold_of(FOLD_YE, s_inv[KEEP_Y], s_inv[KEEP_E]);
+            } else if (w == 2) {
+                fold_of(FOLD_YS, s_inv[KEEP_Y], s_inv[KEEP_S]);
+            } else {
+                fold_of(FOLD_ED, s_inv[KEEP_E], s_inv[KEEP_DS]);
             }
-            top = fminf(wave_max(top), 0x1p120f);
-            const float r = pow2_inverse(top);
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int i = lane + 64 * j;
-                if (i < DVP) s_fold[wave][col_place(i)] = (_Float16)(x[j] * r);
-            }
-            if (lane == 0) s_top[wave] = top;
         }
-        // S and dS on their way while the 64 x 64 products run
+        // S on its way while the 64 x 64 products run, dS while those with S do
+        // (float32 calls have no registers left for that)
+        constexpr bool EARLY = P == 1;
         constexpr int SP = (Ls::STATE / 16 + NT - 1) / NT;
-        uint4 bS[SP], bD[SP];
+        uint4 bS[EARLY ? SP : 1], bD[EARLY ? SP : 1];
+        auto fetch = [&](uint4* x, const uint4* from) {
+            if (EARLY)
 #pragma unroll
-        for (int j = 0; j < SP; ++j) {
-            const int i = min(tid + NT * j, Ls::STATE / 16 - 1);
-            bS[j] = gS[i];
-            bD[j] = gD[i];
-        }
+                for (int j = 0; j < SP; ++j) x[j] = from[min(tid + NT * j, Ls::STATE / 16 - 1)];
+        };
+        auto put = [&](const uint4* x, const uint4* from) {
+            if (EARLY) {
+#pragma unroll
+                for (int j = 0; j < SP; ++j)
+                    if (tid + NT * j < Ls::STATE / 16)
+                        reinterpret_cast<uint4*>(reg)[tid + NT * j] = x[j];
+            } else {
+#pragma unroll 2
+                for (int i = tid; i < Ls::STATE / 16; i += NT)
+                    reinterpret_cast<uint4*>(reg)[i] = from[i];
+            }
+        };
+        fetch(bS, gS);
         __syncthreads();
         auto folded = [&](const Operand<P, VS>& x, int f) {
             Operand<P, VS> y;
@@ -584,7 +616,6 @@ __global__ __launch_bounds__(512) void gdr_grad_kernel(const GradArgs<T> ga)
                     ee.lo[s] = rows_frag(reg + Ls::ROWS / 2, w, s);
                     ye.lo[s] = rows_frag(reg + Ls::ROWS + Ls::ROWS / 2, w, s);
                 }
-                if (half == 0)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const int i = 32 * s + 4 * gq + (e & 3) + 16 * (e >> 2);
@@ -597,35 +628,32 @@ __global__ __launch_bounds__(512) void gdr_grad_kernel(const GradArgs<T> ga)
                         x += (y * s_inv[KEEP_Y][i]) * (z * s_inv[KEEP_E][i]);
                     }
             }
-            if (half == 0) {
-                x = column_sum(x);
-                if (gq == 0 && row < len) ga.dbeta[(size_t)(c0 + row) * a.H + h] = from_f32<T>(x);
-            }
+            x = column_sum(x);
+            if (gq == 0 && row < len) ga.dbeta[(size_t)(c0 + row) * a.H + h] = from_f32<T>(x);
         }
-        // C, Z and the pairs' share of the log-decay's gradient: column blocks 2 half, 2 half + 1
+        // C, Z and the pairs' share of the log-decay's gradient
+        floatx4 Ct[Ls::SHARE ? 4 : 1], Zt[Ls::SHARE ? 4 : 1];
         {
             const Operand<P, VS> goE = folded(go, FOLD_E), yeE = folded(ye, FOLD_YE);
             const float top1 = s_top[FOLD_E], top2 = s_top[FOLD_YE];
             float carry[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 1
-            for (int c = 2 * half; c < 2 * half + 2; ++c) {
+#pragma unroll Ls::SHARE ? 4 : 1
+            for (int c = 0; c < 4; ++c) {
                 float cs = 0.f;
                 if (c <= w) {
                     floatx4 kk = zero4(), qk = zero4(), d1 = zero4(), d2 = zero4();
 #pragma unroll
                     for (int i = 0; i < KS; ++i) {
-                        // rows of either block: c and w are not known at compile time
-                        auto frag = [&](int o, int b) {
-                            const int r = (i + KS * b) & 3;
-                            return *reinterpret_cast<const half8*>(
-                                lds + o + (b * KS + i) * 1024 + gq * 256 + ((li + r) & 15) * 16);
+                        auto of_wave = [&](int o) {
+                            return *reinterpret_cast<const half8*>(lds + o + i * 1024 + wrow[i & 3]);
                         };
-                        const half8 kh = frag(Sh::O_K, c), kw = frag(Sh::O_K, w), qw = frag(Sh::O_Q, w);
+                        const half8 kh = frag_rows<KS>(lds + Sh::O_K, lo, c, i), kw = of_wave(Sh::O_K),
+                                    qw = of_wave(Sh::O_Q);
                         half8 kl = kh, kwl = kw, qwl = qw;
                         if (P == 2) {
-                            kl = frag(Sh::O_K + Sh::RB, c);
-                            kwl = frag(Sh::O_K + Sh::RB, w);
-                            qwl = frag(Sh::O_Q + Sh::RB, w);
+                            kl = frag_rows<KS>(lds + Sh::O_K + Sh::RB, lo, c, i);
+                            kwl = of_wave(Sh::O_K + Sh::RB);
+                            qwl = of_wave(Sh::O_Q + Sh::RB);
                         }
                         kk = mma_parts<P>(kw, kwl, kh, kl, kk);
                         qk = mma_parts<P>(qw, qwl, kh, kl, qk);
@@ -648,8 +676,13 @@ __global__ __launch_bounds__(512) void gdr_grad_kernel(const GradArgs<T> ga)
                             t >= s ? bs * __builtin_amdgcn_exp2f((float)(s_l[t] - ls)) : 0.f;
                         const float cc = t >= s ? a.scale * rho * (d1[r] * top1 * s_ri[t]) : 0.f;
                         const float zz = t > s ? -s_be[t] * rho * (d2[r] * top2) : 0.f;
-                        if (t >= s) sC[t * CP + s] = cc;
-                        if (t > s) sC[s * CP + t] = zz;
+                        if (Ls::SHARE) {
+                            Ct[c][r] = cc;
+                            Zt[c][r] = zz;
+                        } else {
+                            if (t >= s) sC[t * CP + s] = cc;
+                            if (t > s) sC[s * CP + t] = zz;
+                        }
                         const float p = (cc * (qk[r] * s_qs[t]) + zz * (kk[r] * s_ks[t])) * ks;
                         // what stands before place s in the row, down the column from the diagonal
                         const float before = carry[r] + before16(p);
@@ -660,46 +693,20 @@ __global__ __launch_bounds__(512) void gdr_grad_kernel(const GradArgs<T> ga)
                 cs = column_sum(cs);
                 if (gq == 0) s_cross[w][16 * c + li] = cs;
             }
-            if (half == 0 && li == 0)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) s_tot[16 * w + 4 * gq + r] = carry[r];
         }
-        // <S, dS>, then both to LDS
-        float dot = 0.f;
+        if (Ls::SHARE) {
+            __syncthreads();  // E and Y are read
 #pragma unroll
-        for (int j = 0; j < SP; ++j) {
-            const int i = tid + NT * j;
-            if (i >= Ls::STATE / 16 / P) continue;  // P = 2: with the low halves, read here
-            const half8 sh = __builtin_bit_cast(half8, bS[j]), dh = __builtin_bit_cast(half8, bD[j]);
-            float x = 0.f;
-            half8 sl = sh, dl = dh;
-            if (P == 2) {
-                sl = __builtin_bit_cast(half8, gS[i + Ls::STATE / 32]);
-                dl = __builtin_bit_cast(half8, gD[i + Ls::STATE / 32]);
-            }
+            for (int c = 0; c < 4; ++c)
+                if (c <= w)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                float y = (float)sh[e], z = (float)dh[e];
-                if (P == 2) {
-                    y += (float)sl[e];
-                    z += (float)dl[e];
-                }
-                x += y * z;
-            }
-            const int col = i / (64 * KS) * 16 + (i & 15);
-            dot += (x * s_inv[KEEP_S][col]) * s_inv[KEEP_DS][col];
+                    for (int r = 0; r < 4; ++r) {
+                        const int t = 16 * w + 4 * gq + r, s = 16 * c + li;
+                        if (t >= s) sC[t * CP + s] = Ct[c][r];
+                        if (t > s) sC[s * CP + t] = Zt[c][r];
+                    }
         }
-        dot = wave_sum(dot);
-        if (lane == 0) s_dot[wave] = dot;
-        __syncthreads();  // E and Y are read, C and Z written
-#pragma unroll
-        for (int j = 0; j < SP; ++j) {
-            const int i = tid + NT * j;
-            if (i < Ls::STATE / 16) {
-                reinterpret_cast<uint4*>(reg)[i] = bS[j];
-                if (Ls::BOTH) reinterpret_cast<uint4*>(reg + Ls::STATE)[i] = bD[j];
-            }
-        }
+        __syncthreads();
         // C's rows, its columns and the rows of Z + Z^T as operands, over the scales of the K or Q rows
         // that they meet
         Operand<P, 2> opC, opT, opZ;
@@ -732,12 +739,15 @@ __global__ __launch_bounds__(512) void gdr_grad_kernel(const GradArgs<T> ga)
                         for (int e = 0; e < 8; ++e) op.lo[s][e] = (_Float16)(y[s][e] - (float)op.hi[s][e]);
                     }
                 }
-                if (gq == 0) out[row] = inv;  // both halves of the key channels write the same
+                if (gq == 0) out[row] = inv;
             };
             convert(x[0], m[0], opC, s_ic);
             convert(x[1], m[1], opT, s_it);
             convert(x[2], m[2], opZ, s_iz);
         }
+        __syncthreads();  // C and Z are read
+        put(bS, gS);
+        fetch(bD, gD);
         __syncthreads();
 
         // products over the value columns, and the small ones, per 16 key channels
@@ -754,9 +764,7 @@ __global__ __launch_bounds__(512) void gdr_grad_kernel(const GradArgs<T> ga)
         }
         // q or k of the result tile's places: four tokens of a channel
         auto four = [&](int o, int k, float* y) {
-            const int b = w, rot = ((k >> 1) + KS * b) & 3;
-            const char* p = lds + o + (b * KS + (k >> 1)) * 1024 + (k & 1) * 8 + (li & 3) * 256 +
-                            ((4 * gq + (li >> 2) + rot) & 15) * 16;
+            const char* p = lds + o + (k >> 1) * 1024 + (k & 1) * 8 + wtr[(k >> 1) & 3];
             const half4 x = lds_read_tr(p);
             half4 z = x;
             if (P == 2) z = lds_read_tr(p + Sh::RB);
@@ -766,9 +774,8 @@ __global__ __launch_bounds__(512) void gdr_grad_kernel(const GradArgs<T> ga)
         {
             const Operand<P, VS> goS = folded(go, FOLD_S), yeS = folded(ye, FOLD_YS);
 #pragma unroll
-            for (int j = 0; j < KH; ++j) {
-                const int k = half * KH + j;
-                if (k >= KT) continue;
+            for (int k = 0; k < KT; ++k) {
+                if (P == 1) __builtin_amdgcn_sched_barrier(0);  // no tile's reads ahead of the one before
                 floatx4 p1 = zero4(), p2 = zero4();
 #pragma unroll
                 for (int s = 0; s < VS; ++s) {
@@ -781,16 +788,7 @@ __global__ __launch_bounds__(512) void gdr_grad_kernel(const GradArgs<T> ga)
                 floatx4 a1 = zero4(), a2 = zero4(), a3 = zero4();
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
-                    auto cols = [&](int o) {  // frag_cols with k known at run time
-                        half4 x[2];
-#pragma unroll
-                        for (int u = 0; u < 2; ++u) {
-                            const int b = 2 * s + u, rot = ((k >> 1) + KS * b) & 3;
-                            x[u] = lds_read_tr(lds + o + (b * KS + (k >> 1)) * 1024 + (k & 1) * 8 +
-                                               (li & 3) * 256 + ((4 * gq + (li >> 2) + rot) & 15) * 16);
-                        }
-                        return __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7);
-                    };
+                    auto cols = [&](int o) { return frag_cols<KS>(lds + o, lo, k, s); };
                     const half8 kh = cols(Sh::O_K), qh = cols(Sh::O_Q);
                     half8 kl = kh, ql = qh;
                     if (P == 2) {
@@ -809,27 +807,55 @@ __global__ __launch_bounds__(512) void gdr_grad_kernel(const GradArgs<T> ga)
                     const int t = 16 * w + 4 * gq + r;
                     const float x1 = rq[r] * p1[r], x2 = rk[r] * p2[r];
                     reads[r] += (qv[r] * s_qs[t]) * x1 + (kv[r] * s_ks[t]) * x2;
-                    dq[j][r] += x1 + a1[r] * s_ic[t];
-                    dk[j][r] += x2 + (a2[r] * s_it[t] + a3[r] * s_iz[t]);
+                    dq[k][r] += x1 + a1[r] * s_ic[t];
+                    dk[k][r] += x2 + (a2[r] * s_it[t] + a3[r] * s_iz[t]);
                 }
+                // the tile's sums end here: put off to the last tile's, their terms fill the registers
+                asm volatile("" : "+v"(dq[k]), "+v"(dk[k]));
+                asm volatile("" : "+v"(reads[0]), "+v"(reads[1]), "+v"(reads[2]), "+v"(reads[3]));
             }
         }
-        if (!Ls::BOTH) {
-            __syncthreads();
+        // <S, dS>
+        float dot = 0.f;
+        auto dot_of = [&](int i, half8 dh) {
+            if (i >= Ls::STATE / 16 / P) return;  // float32 calls: the low halves with the high ones
+            const half8 sh = reinterpret_cast<const half8*>(reg)[i];
+            half8 sl = sh, dl = dh;
+            if (P == 2) {
+                sl = reinterpret_cast<const half8*>(reg)[i + Ls::STATE / 32];
+                dl = __builtin_bit_cast(half8, gD[i + Ls::STATE / 32]);
+            }
+            float x = 0.f;
 #pragma unroll
-            for (int j = 0; j < SP; ++j) {
-                const int i = tid + NT * j;
-                if (i < Ls::STATE / 16) reinterpret_cast<uint4*>(reg)[i] = bD[j];
+            for (int e = 0; e < 8; ++e) {
+                float y = (float)sh[e], z = (float)dh[e];
+                if (P == 2) {
+                    y += (float)sl[e];
+                    z += (float)dl[e];
+                }
+                x += y * z;
             }
-            __syncthreads();
+            const int col = i / (64 * KS) * 16 + (i & 15);
+            dot += (x * s_inv[KEEP_S][col]) * s_inv[KEEP_DS][col];
+        };
+        if (EARLY) {
+#pragma unroll
+            for (int j = 0; j < SP; ++j) dot_of(tid + NT * j, __builtin_bit_cast(half8, bD[j]));
+        } else {
+#pragma unroll 1
+            for (int i = tid; i < Ls::STATE / 32; i += NT) dot_of(i, __builtin_bit_cast(half8, gD[i]));
         }
+        dot = wave_sum(dot);
+        if (lane == 0) s_dot[w] = dot;
+        __syncthreads();  // S is read
+        put(bD, gD);
+        __syncthreads();
         {
-            const char* D = Ls::BOTH ? reg + Ls::STATE : reg;
+            const char* D = reg;
             const Operand<P, VS> eeD = folded(ee, FOLD_ED);
 #pragma unroll
-            for (int j = 0; j < KH; ++j) {
-                const int k = half * KH + j;
-                if (k >= KT) continue;
+            for (int k = 0; k < KT; ++k) {
+                if (P == 1) __builtin_amdgcn_sched_barrier(0);
                 floatx4 p3 = zero4();
 #pragma unroll
                 for (int s = 0; s < VS; ++s) {
@@ -844,39 +870,36 @@ __global__ __launch_bounds__(512) void gdr_grad_kernel(const GradArgs<T> ga)
                 for (int r = 0; r < 4; ++r) {
                     const float x3 = rt[r] * p3[r];
                     writes[r] += (kv[r] * s_ks[16 * w + 4 * gq + r]) * x3;
-                    dk[j][r] += x3;
+                    dk[k][r] += x3;
                 }
+                asm volatile("" : "+v"(dk[k]));
+                asm volatile("" : "+v"(writes[0]), "+v"(writes[1]), "+v"(writes[2]), "+v"(writes[3]));
             }
         }
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const float x = row16_sum(reads[r]), y = row16_sum(writes[r]);
             if (li == 0) {
-                s_reads[half][16 * w + 4 * gq + r] = x;
-                s_writes[half][16 * w + 4 * gq + r] = y;
+                s_reads[16 * w + 4 * gq + r] = x;
+                s_writes[16 * w + 4 * gq + r] = y;
             }
         }
         __syncthreads();
-        if (wave == 0) {  // lane = token
-            float after = s_reads[0][lane] + s_reads[1][lane], before = s_writes[0][lane] + s_writes[1][lane];
-            float tot = s_tot[lane];
+        if (w == 0) {  // lane = token
+            float after = s_reads[lane], before = s_writes[lane];
 #pragma unroll
             for (int off = 1; off < 64; off <<= 1) {
                 const float x = __shfl_down(after, off, 64), y = __shfl_up(before, off, 64);
-                const float z = __shfl_down(tot, off, 64);
-                if (lane + off < 64) {
-                    after += x;
-                    tot += z;
-                }
+                if (lane + off < 64) after += x;
                 if (lane >= off) before += y;
             }
             before = __shfl_up(before, 1, 64);  // of the tokens before this one
             if (lane == 0) before = 0.f;
-            float cross = lane >= 32 ? tot : 0.f;  // the column blocks of the other half
+            float cross = 0.f;
             for (int b = 0; b < 4; ++b) cross += s_cross[b][lane];
             float whole = 0.f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) whole += s_dot[i];
+            for (int i = 0; i < 4; ++i) whole += s_dot[i];
             const float dlog = cross + after + before + fac[REC_FACTORS] * whole;
             if (lane < len) {
                 const size_t at = (size_t)(c0 + lane) * a.H + h;
@@ -885,19 +908,14 @@ __global__ __launch_bounds__(512) void gdr_grad_kernel(const GradArgs<T> ga)
         }
         __syncthreads();
     }
+    const int gq = (thread & 63) >> 4, li = thread & 15, j = li & 3, t = 16 * (thread >> 6) + 4 * gq + j;
+    const size_t at = ((size_t)(c0 + t) * a.Hk + hk) * DK + (li & ~3);
 #pragma unroll
-    for (int j = 0; j < KH; ++j) {
-        const int k = half * KH + j;
-        if (k >= KT) continue;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int t = 16 * w + 4 * gq + r;
-            if (t < len) {
-                const size_t at = ((size_t)(c0 + t) * a.Hk + hk) * DK + 16 * k + li;
-                ga.dq[at] = from_f32<T>(dq[j][r]);
-                ga.dk[at] = from_f32<T>(dk[j][r]);
-            }
-        }
+    for (int k = 0; k < KT; ++k) {
+        const float x[4] = {dq[k][0], dq[k][1], dq[k][2], dq[k][3]};
+        const float y[4] = {dk[k][0], dk[k][1], dk[k][2], dk[k][3]};
+        store_quad<T>(reinterpret_cast<char*>(ga.dq + at + 16 * k), t < len, j, x);
+        store_quad<T>(reinterpret_cast<char*>(ga.dk + at + 16 * k), t < len, j, y);
     }
 }
 
@@ -911,7 +929,7 @@ hipError_t launch_rest(const GradArgs<T>& ga, hipStream_t stream)
                        stream, ga);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((gdr_grad_kernel<T, DK, DV>), dim3((unsigned)(a.maxch * a.Hk)), dim3(512), 0,
+    hipLaunchKernelGGL((gdr_grad_kernel<T, DK, DV>), dim3((unsigned)(a.maxch * a.Hk)), dim3(256), 0,
                        stream, ga);
     return hipGetLastError();
 }

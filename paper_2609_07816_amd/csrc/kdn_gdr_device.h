@@ -421,53 +421,57 @@ struct Loader {
     }
 };
 
-// Stores a lane's 16 values of a column of [tokens][H][DV] (result tile layout: rows 16b + 4g + r of
-// column i), step bytes from token to token, of a chunk of len tokens. Four lanes of adjacent columns
-// exchange their four rows (a transpose within each quad), so that each stores four adjacent columns of
-// one row: 4 stores of 8 (float32: 16) bytes in place of 16 of 2 (4). base: the chunk's first token at the
-// wave's first column.
 template <int S>
 __device__ __forceinline__ unsigned quad_lane(unsigned x)  // of lane S of this lane's quad
 {
     return (unsigned)__builtin_amdgcn_mov_dpp((int)x, S * 0x55, 0xf, 0xf, true);
 }
+
+// Four lanes of adjacent columns hold four rows each of their column (x[0 .. 3]); lane j of the quad
+// stores row j of the four columns at `at`: one store of 8 (float32: 16) bytes in place of 4 of 2 (4).
+template <class T>
+__device__ __forceinline__ void store_quad(char* at, bool in, int j, const float* x)
+{
+    if constexpr (sizeof(T) == 2) {
+        const bf16x4 y = {(bf16)x[0], (bf16)x[1], (bf16)x[2], (bf16)x[3]};
+        const uint2 z = __builtin_bit_cast(uint2, y);  // rows 0 and 1, 2 and 3
+        // this lane's row of the quad's lanes: the pair by j / 2, its half by j % 2
+        const unsigned half = j & 1 ? 0x07060302u : 0x05040100u;
+        const unsigned x0 = quad_lane<0>(z.x), y0 = quad_lane<0>(z.y);
+        const unsigned x1 = quad_lane<1>(z.x), y1 = quad_lane<1>(z.y);
+        const unsigned x2 = quad_lane<2>(z.x), y2 = quad_lane<2>(z.y);
+        const unsigned x3 = quad_lane<3>(z.x), y3 = quad_lane<3>(z.y);
+        const unsigned v0 = j < 2 ? x0 : y0, v1 = j < 2 ? x1 : y1;
+        const unsigned v2 = j < 2 ? x2 : y2, v3 = j < 2 ? x3 : y3;
+        const uint2 out = make_uint2(__builtin_amdgcn_perm(v1, v0, half),
+                                     __builtin_amdgcn_perm(v3, v2, half));
+        if (in) *reinterpret_cast<uint2*>(at) = out;
+    } else {
+        unsigned z[4], v[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) z[r] = __float_as_uint(x[r]);
+        auto mine = [&](unsigned a, unsigned b, unsigned c, unsigned d) {
+            const unsigned ab = j & 1 ? b : a, cd = j & 1 ? d : c;
+            return j & 2 ? cd : ab;
+        };
+        v[0] = mine(quad_lane<0>(z[0]), quad_lane<0>(z[1]), quad_lane<0>(z[2]), quad_lane<0>(z[3]));
+        v[1] = mine(quad_lane<1>(z[0]), quad_lane<1>(z[1]), quad_lane<1>(z[2]), quad_lane<1>(z[3]));
+        v[2] = mine(quad_lane<2>(z[0]), quad_lane<2>(z[1]), quad_lane<2>(z[2]), quad_lane<2>(z[3]));
+        v[3] = mine(quad_lane<3>(z[0]), quad_lane<3>(z[1]), quad_lane<3>(z[2]), quad_lane<3>(z[3]));
+        if (in) *reinterpret_cast<uint4*>(at) = make_uint4(v[0], v[1], v[2], v[3]);
+    }
+}
+// Stores a lane's 16 values of a column of [tokens][H][DV] (result tile layout: rows 16b + 4g + r of
+// column i), step bytes from token to token, of a chunk of len tokens. base: the chunk's first token at
+// the wave's first column.
 template <class T>
 __device__ __forceinline__ void store_tile(T* base, unsigned step, int lane, int len, const float* x)
 {
     const int gq = lane >> 4, li = lane & 15, j = li & 3;
     char* p = reinterpret_cast<char*>(base) + (unsigned)(4 * gq + j) * step + (li & ~3) * sizeof(T);
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
-        const bool in = 16 * b + 4 * gq + j < len;
-        char* at = p + (size_t)(16 * b) * step;
-        if constexpr (sizeof(T) == 2) {
-            const bf16x4 y = {(bf16)x[4 * b], (bf16)x[4 * b + 1], (bf16)x[4 * b + 2], (bf16)x[4 * b + 3]};
-            const uint2 z = __builtin_bit_cast(uint2, y);  // rows 0 and 1, 2 and 3
-            // this lane's row of the quad's lanes: the pair by j / 2, its half by j % 2
-            const unsigned half = j & 1 ? 0x07060302u : 0x05040100u;
-            const unsigned x0 = quad_lane<0>(z.x), y0 = quad_lane<0>(z.y);
-            const unsigned x1 = quad_lane<1>(z.x), y1 = quad_lane<1>(z.y);
-            const unsigned x2 = quad_lane<2>(z.x), y2 = quad_lane<2>(z.y);
-            const unsigned x3 = quad_lane<3>(z.x), y3 = quad_lane<3>(z.y);
-            const unsigned v0 = j < 2 ? x0 : y0, v1 = j < 2 ? x1 : y1;
-            const unsigned v2 = j < 2 ? x2 : y2, v3 = j < 2 ? x3 : y3;
-            const uint2 out = make_uint2(__builtin_amdgcn_perm(v1, v0, half),
-                                         __builtin_amdgcn_perm(v3, v2, half));
-            if (in) *reinterpret_cast<uint2*>(at) = out;
-        } else {
-            unsigned z[4], v[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) z[r] = __float_as_uint(x[4 * b + r]);
-            auto mine = [&](unsigned a, unsigned b, unsigned c, unsigned d) {
-                return j < 2 ? (j == 0 ? a : b) : (j == 2 ? c : d);
-            };
-            v[0] = mine(quad_lane<0>(z[0]), quad_lane<0>(z[1]), quad_lane<0>(z[2]), quad_lane<0>(z[3]));
-            v[1] = mine(quad_lane<1>(z[0]), quad_lane<1>(z[1]), quad_lane<1>(z[2]), quad_lane<1>(z[3]));
-            v[2] = mine(quad_lane<2>(z[0]), quad_lane<2>(z[1]), quad_lane<2>(z[2]), quad_lane<2>(z[3]));
-            v[3] = mine(quad_lane<3>(z[0]), quad_lane<3>(z[1]), quad_lane<3>(z[2]), quad_lane<3>(z[3]));
-            if (in) *reinterpret_cast<uint4*>(at) = make_uint4(v[0], v[1], v[2], v[3]);
-        }
-    }
+    for (int b = 0; b < 4; ++b)
+        store_quad<T>(p + (size_t)(16 * b) * step, 16 * b + 4 * gq + j < len, j, x + 4 * b);
 }
 
 // Keeps what stands before it (requests of operands) before what stands after it (the products and
