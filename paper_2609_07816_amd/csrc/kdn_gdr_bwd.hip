@@ -570,29 +570,29 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void gdr_grad_kernel(c
                 fold_of(FOLD_ED, s_inv[KEEP_E], s_inv[KEEP_DS]);
             }
         }
-        // S on its way while the 64 x 64 products run, dS while those with S do
+        // S on its way while C and Z become operands, dS while the products with S run
         // (float32 calls have no registers left for that)
         constexpr bool EARLY = P == 1;
         constexpr int SP = (Ls::STATE / 16 + NT - 1) / NT;
-        uint4 bS[EARLY ? SP : 1], bD[EARLY ? SP : 1];
-        auto fetch = [&](uint4* x, const uint4* from) {
-            if (EARLY)
-#pragma unroll
-                for (int j = 0; j < SP; ++j) x[j] = from[min(tid + NT * j, Ls::STATE / 16 - 1)];
-        };
-        auto put = [&](const uint4* x, const uint4* from) {
-            if (EARLY) {
+        half8 bS[EARLY ? SP : 1], bD[EARLY ? SP : 1];
+        auto fetch = [&](auto& x, const uint4* from) {
+            if constexpr (EARLY)
 #pragma unroll
                 for (int j = 0; j < SP; ++j)
-                    if (tid + NT * j < Ls::STATE / 16)
-                        reinterpret_cast<uint4*>(reg)[tid + NT * j] = x[j];
+                    x[j] = reinterpret_cast<const half8*>(from)[min(tid + NT * j, Ls::STATE / 16 - 1)];
+        };
+        auto put = [&](const auto& x, const uint4* from) {
+            if constexpr (EARLY) {
+#pragma unroll
+                for (int j = 0; j < SP; ++j)
+                    if (Ls::STATE / 16 % NT == 0 || tid + NT * j < Ls::STATE / 16)
+                        reinterpret_cast<half8*>(reg)[tid + NT * j] = x[j];
             } else {
 #pragma unroll 2
                 for (int i = tid; i < Ls::STATE / 16; i += NT)
                     reinterpret_cast<uint4*>(reg)[i] = from[i];
             }
         };
-        fetch(bS, gS);
         __syncthreads();
         auto folded = [&](const Operand<P, VS>& x, int f) {
             Operand<P, VS> y;
@@ -694,6 +694,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void gdr_grad_kernel(c
                 if (gq == 0) s_cross[w][16 * c + li] = cs;
             }
         }
+        fetch(bS, gS);
         if (Ls::SHARE) {
             __syncthreads();  // E and Y are read
 #pragma unroll
@@ -840,7 +841,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void gdr_grad_kernel(c
         };
         if (EARLY) {
 #pragma unroll
-            for (int j = 0; j < SP; ++j) dot_of(tid + NT * j, __builtin_bit_cast(half8, bD[j]));
+            for (int j = 0; j < SP; ++j) dot_of(tid + NT * j, bD[j]);
         } else {
 #pragma unroll 1
             for (int i = tid; i < Ls::STATE / 32; i += NT) dot_of(i, __builtin_bit_cast(half8, gD[i]));
