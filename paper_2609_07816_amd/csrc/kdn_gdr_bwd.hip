@@ -354,7 +354,7 @@ __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_reverse_kernel(const Gra
 // ------------------------------------------------------------------------------------------
 // gdr_grad: a workgroup of four waves per (chunk, key head), wave w has tokens 16w .. 16w+15; the value
 // heads of the key head one after another, dQ and dK summed in registers in that order. E and Y, then C
-// and Z, then S, then dS come through one region of LDS (70 KB in all at d 128 in bf16: two workgroups on
+// and Z over Y, then S, then dS come through one region of LDS (74 KB in all at d 128 in bf16: two workgroups on
 // a CU, whose waits overlap), from where the transposing read gives either side's fragments; the scales
 // of the value columns, over which the products contract, are folded into the A side (each over the
 // largest).
@@ -402,15 +402,55 @@ struct GradLds {
     static constexpr int P = Sh::P;
     static constexpr int ROWS = (int)keep_rows<T>(DV) * 2;        // bytes of E or Y
     static constexpr int STATE = (int)keep_state<T, DK>(DV) * 2;  // of S or dS
-    static constexpr int MATRIX = 64 * 68 * 4;                    // C and Z
-    static constexpr int R0 = 2 * ROWS > STATE ? 2 * ROWS : STATE;
-    // float32 calls, which are alone on their CU as it is, keep C and Z in a place of their own and so
-    // out of the registers
-    static constexpr bool SHARE = P == 1;
-    static constexpr int R = !SHARE ? R0 + MATRIX : R0 > MATRIX ? R0 : MATRIX;
+    static constexpr int MATRIX = 64 * 68 * 4;                    // C and Z, over Y and what follows it
+    static constexpr int R0 = ROWS + (ROWS > MATRIX ? ROWS : MATRIX);
+    static constexpr int R = R0 > STATE ? R0 : STATE;
 };
 
 constexpr int CP = 68;  // floats of a row of the 64 x 64 matrix in LDS
+
+// What a value head brings first, in registers: all of it is on its way at once, for the first head with
+// K and Q (one after another the round trips were most of the kernel's time).
+template <class T, int DV>
+struct GradStage {
+    static constexpr int NT = 256, VS = DV < 32 ? 1 : DV / 32, VT = DV / 16;
+    static constexpr int N = (int)keep_rows<T>(DV) * 2 / 16;  // pieces of 16 bytes of E or Y
+    static constexpr int RP = (N + NT - 1) / NT, SP = (KEEP_COUNT * DV + NT - 1) / NT;
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    half8 e[RP], y[RP];
+    T4 d[VS][2];
+    float scale[SP], be, gate, last;
+    double l;
+
+    __device__ __forceinline__ void fetch(const GradArgs<T>& ga, size_t kept, const char* rec, int h, int c0,
+                                          int len, int tid)
+    {
+        const half8* gE = reinterpret_cast<const half8*>(ga.keep.E + kept * keep_rows<T>(DV));
+        const half8* gY = reinterpret_cast<const half8*>(ga.keep.Y + kept * keep_rows<T>(DV));
+#pragma unroll
+        for (int j = 0; j < RP; ++j) {
+            e[j] = gE[min(tid + NT * j, N - 1)];
+            y[j] = gY[min(tid + NT * j, N - 1)];
+        }
+        const float* fac = reinterpret_cast<const float*>(rec);
+        l = reinterpret_cast<const double*>(fac + F_L * GC)[tid % GC];
+        be = fac[F_BE * GC + tid % GC];
+        last = fac[REC_FACTORS];
+        gate = to_f32(ga.c.alpha[(size_t)(c0 + min(tid % GC, len - 1)) * ga.c.H + h]);
+#pragma unroll
+        for (int j = 0; j < SP; ++j)
+            scale[j] = ga.keep.scale[kept * KEEP_COUNT * DV + min(tid + NT * j, KEEP_COUNT * DV - 1)];
+        // dO: this wave's rows
+        const int row = 16 * (tid >> 6) + (tid & 15);
+        const T* from = ga.dO ? ga.dO : ga.c.v;  // with no dO: loads of the same shape, not used
+        const T* p = from + ((size_t)(c0 + min(row, len - 1)) * ga.c.H + h) * DV + 4 * ((tid & 63) >> 4);
+#pragma unroll
+        for (int s = 0; s < VS; ++s)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                d[s][u] = *reinterpret_cast<const T4*>(p + 32 * s + (VT > 1 ? 16 * u : 0));
+    }
+};
 
 template <class T, int DK, int DV>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void gdr_grad_kernel(const GradArgs<T> ga)
@@ -423,8 +463,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void gdr_grad_kernel(c
     constexpr int DVP = VS * 32;
     const ChunkArgs<T>& a = ga.c;
     __shared__ __align__(16) char lds[Sh::BYTES];     // K, Q
-    __shared__ __align__(16) char reg[Ls::R];         // E and Y; C and Z; S; dS
-    float* sC = reinterpret_cast<float*>(reg + (Ls::SHARE ? 0 : Ls::R0));        // C on and below the diagonal, Z^T above it
+    __shared__ __align__(16) char reg[Ls::R];         // E and Y; E, C and Z; S; dS
+    float* sC = reinterpret_cast<float*>(reg + Ls::ROWS);        // C on and below the diagonal, Z^T above it
     __shared__ __align__(16) _Float16 s_fold[FOLD_COUNT][DVP];
     __shared__ float s_top[FOLD_COUNT], s_inv[KEEP_COUNT][DV];
     __shared__ double s_l[GC];
@@ -440,18 +480,6 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void gdr_grad_kernel(c
         for (int i = thread; i < Sh::BYTES / 16; i += NT)
             reinterpret_cast<uint4*>(lds)[i] = make_uint4(0, 0, 0, 0);
         __syncthreads();
-    }
-    const char* rec = a.rec + ((size_t)g * a.H + (size_t)hk * a.rep) * REC;
-    {
-        Loader<T, DK, Sh, NT, 0> ld;
-        const size_t at = ((size_t)c0 * a.Hk + hk) * DK;
-        ld.load(a.k + at, a.q + at, (unsigned)(a.Hk * DK * sizeof(T)), thread, len, rec);
-        ld.store(lds, thread);
-        const float* fac = reinterpret_cast<const float*>(rec);
-        if (thread < GC) {  // 0 for the tokens past the end, as the rows' scales
-            s_ks[thread] = fac[F_KS * GC + thread] > 0.f ? pow2_inverse(fac[F_KS * GC + thread]) : 0.f;
-            s_qs[thread] = fac[F_QS * GC + thread] > 0.f ? pow2_inverse(fac[F_QS * GC + thread]) : 0.f;
-        }
     }
     floatx4 dq[KT], dk[KT];
 #pragma unroll
@@ -490,39 +518,51 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void gdr_grad_kernel(c
             const half4 z = VT > 1 ? lds_read_tr(p + (2 * s + 1) * KS * 1024) : half4{0, 0, 0, 0};
             return __builtin_shufflevector(y, z, 0, 1, 2, 3, 4, 5, 6, 7);
         };
-        rec = a.rec + kept * REC;
-        const float* fac = reinterpret_cast<const float*>(rec);
-        const uint4* gE = reinterpret_cast<const uint4*>(ga.keep.E + kept * keep_rows<T>(DV));
-        const uint4* gY = reinterpret_cast<const uint4*>(ga.keep.Y + kept * keep_rows<T>(DV));
+        const char* rec = a.rec + kept * REC;
         const uint4* gS = reinterpret_cast<const uint4*>(ga.keep.S + kept * keep_state<T, DK>(DV));
         const uint4* gD = reinterpret_cast<const uint4*>(ga.keep.dS + kept * keep_state<T, DK>(DV));
-        for (int i = tid; i < Ls::ROWS / 16; i += NT) {
-            reinterpret_cast<uint4*>(reg)[i] = gE[i];
-            reinterpret_cast<uint4*>(reg + Ls::ROWS)[i] = gY[i];
+        using St = GradStage<T, DV>;
+        St stage;
+        if (hv == 0) {
+            Loader<T, DK, Sh, NT, 0> ld;
+            const size_t at = ((size_t)c0 * a.Hk + hk) * DK;
+            ld.load(a.k + at, a.q + at, (unsigned)(a.Hk * DK * sizeof(T)), tid, len, rec);
+            const float* fac = reinterpret_cast<const float*>(rec);
+            const float ks = fac[F_KS * GC + tid % GC], qs = fac[F_QS * GC + tid % GC];
+            stage.fetch(ga, kept, rec, h, c0, len, tid);
+            ld.store(lds, tid);
+            if (tid < GC) {  // 0 for the tokens past the end, as the rows' scales
+                s_ks[tid] = ks > 0.f ? pow2_inverse(ks) : 0.f;
+                s_qs[tid] = qs > 0.f ? pow2_inverse(qs) : 0.f;
+            }
+        } else {
+            stage.fetch(ga, kept, rec, h, c0, len, tid);
         }
+        const float gate = stage.gate, last = stage.last;  // of token lane (wave 0)
+#pragma unroll
+        for (int j = 0; j < St::RP; ++j)
+            if (St::N % NT == 0 || tid + NT * j < St::N) {
+                reinterpret_cast<half8*>(reg)[tid + NT * j] = stage.e[j];
+                reinterpret_cast<half8*>(reg + Ls::ROWS)[tid + NT * j] = stage.y[j];
+            }
         if (tid < GC) {
-            s_l[tid] = reinterpret_cast<const double*>(fac + F_L * GC)[tid];
-            s_be[tid] = fac[F_BE * GC + tid];
+            s_l[tid] = stage.l;
+            s_be[tid] = stage.be;
         }
-        for (int i = tid; i < KEEP_COUNT * DV; i += NT)
-            s_inv[i / DV][i % DV] = ga.keep.scale[kept * KEEP_COUNT * DV + i];
+#pragma unroll
+        for (int j = 0; j < St::SP; ++j)
+            if (tid + NT * j < KEEP_COUNT * DV) s_inv[(tid + NT * j) / DV][(tid + NT * j) % DV] = stage.scale[j];
         // this wave's rows of dO, scaled by row (the inverse scales to s_ri)
         Operand<P, VS> go;
         {
             float x[VS][8], m = 0.f;
-            const T* p = ga.dO + ((size_t)(c0 + min(row, len - 1)) * a.H + h) * DV + 4 * gq;
+            const int have = ga.dO ? len : 0;
 #pragma unroll
             for (int s = 0; s < VS; ++s)
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    struct alignas(4 * sizeof(T)) V4 { T v[4]; };
-                    V4 y = {};
-                    if (ga.dO && (u == 0 || VT > 1)) y = *reinterpret_cast<const V4*>(p + 32 * s + 16 * u);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        x[s][4 * u + e] = row < len ? to_f32(y.v[e]) : 0.f;
-                        m = fmaxf(m, fabsf(x[s][4 * u + e]));
-                    }
+                for (int e = 0; e < 8; ++e) {
+                    x[s][e] = row < have && (e < 4 || VT > 1) ? to_f32(stage.d[s][e >> 2][e & 3]) : 0.f;
+                    m = fmaxf(m, fabsf(x[s][e]));
                 }
             float sc, inv;
             pow2_scale<0>(column_max(m), sc, inv);
@@ -632,12 +672,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void gdr_grad_kernel(c
             if (gq == 0 && row < len) ga.dbeta[(size_t)(c0 + row) * a.H + h] = from_f32<T>(x);
         }
         // C, Z and the pairs' share of the log-decay's gradient
-        floatx4 Ct[Ls::SHARE ? 4 : 1], Zt[Ls::SHARE ? 4 : 1];
+        __syncthreads();  // Y is read
         {
             const Operand<P, VS> goE = folded(go, FOLD_E), yeE = folded(ye, FOLD_YE);
             const float top1 = s_top[FOLD_E], top2 = s_top[FOLD_YE];
             float carry[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll Ls::SHARE ? 4 : 1
+#pragma unroll P == 1 ? 4 : 1
             for (int c = 0; c < 4; ++c) {
                 float cs = 0.f;
                 if (c <= w) {
@@ -676,13 +716,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void gdr_grad_kernel(c
                             t >= s ? bs * __builtin_amdgcn_exp2f((float)(s_l[t] - ls)) : 0.f;
                         const float cc = t >= s ? a.scale * rho * (d1[r] * top1 * s_ri[t]) : 0.f;
                         const float zz = t > s ? -s_be[t] * rho * (d2[r] * top2) : 0.f;
-                        if (Ls::SHARE) {
-                            Ct[c][r] = cc;
-                            Zt[c][r] = zz;
-                        } else {
-                            if (t >= s) sC[t * CP + s] = cc;
-                            if (t > s) sC[s * CP + t] = zz;
-                        }
+                        if (t >= s) sC[t * CP + s] = cc;
+                        if (t > s) sC[s * CP + t] = zz;
                         const float p = (cc * (qk[r] * s_qs[t]) + zz * (kk[r] * s_ks[t])) * ks;
                         // what stands before place s in the row, down the column from the diagonal
                         const float before = carry[r] + before16(p);
@@ -695,18 +730,6 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void gdr_grad_kernel(c
             }
         }
         fetch(bS, gS);
-        if (Ls::SHARE) {
-            __syncthreads();  // E and Y are read
-#pragma unroll
-            for (int c = 0; c < 4; ++c)
-                if (c <= w)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int t = 16 * w + 4 * gq + r, s = 16 * c + li;
-                        if (t >= s) sC[t * CP + s] = Ct[c][r];
-                        if (t > s) sC[s * CP + t] = Zt[c][r];
-                    }
-        }
         __syncthreads();
         // C's rows, its columns and the rows of Z + Z^T as operands, over the scales of the K or Q rows
         // that they meet
@@ -901,10 +924,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void gdr_grad_kernel(c
             float whole = 0.f;
 #pragma unroll
             for (int i = 0; i < 4; ++i) whole += s_dot[i];
-            const float dlog = cross + after + before + fac[REC_FACTORS] * whole;
+            const float dlog = cross + after + before + last * whole;
             if (lane < len) {
                 const size_t at = (size_t)(c0 + lane) * a.H + h;
-                ga.dalpha[at] = from_f32<T>(dlog / fmaxf(to_f32(a.alpha[at]), 0x1p-100f));
+                ga.dalpha[at] = from_f32<T>(dlog / fmaxf(gate, 0x1p-100f));
             }
         }
         __syncthreads();
