@@ -353,10 +353,10 @@ struct Loader {
     static constexpr int RECP = (Lds::REC / 16 + NT - 1) / NT;
     Raw8<T> k[TPT], q[Lds::q ? TPT : 1];
     float4 ks[TPT], qs[Lds::q ? TPT : 1];  // the rows' scales
-    uint4 rec[RECP > 0 ? RECP : 1];
+    half8 rec[RECP > 0 ? RECP : 1];
     static constexpr int VPR = Lds::VCOLS > 0 ? Lds::VCOLS * (int)sizeof(T) / 16 : 1;  // pieces of a row
     static constexpr int VP = Lds::VCOLS > 0 ? (GC * VPR + NT - 1) / NT : 0;          // of V
-    uint4 v[VP > 0 ? VP : 1];
+    half8 v[VP > 0 ? VP : 1];
 
     // The columns at p of V or dO, vstep bytes from token to token. (What is to count as 0 is loaded
     // from elsewhere and dropped at the store: a load in a branch would be waited for behind it.)
@@ -365,7 +365,7 @@ struct Loader {
 #pragma unroll
         for (int j = 0; j < VP; ++j) {
             const int i = (tid + NT * j) % (GC * VPR);
-            v[j] = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(p) +
+            v[j] = *reinterpret_cast<const half8*>(reinterpret_cast<const char*>(p) +
                                                    (unsigned)min(i / VPR, len - 1) * vstep +
                                                    16 * (i % VPR));
         }
@@ -397,7 +397,7 @@ struct Loader {
 #pragma unroll
         for (int j = 0; j < RECP; ++j) {
             const int at = min(tid + NT * j, Lds::REC / 16 - 1);
-            rec[j] = reinterpret_cast<const uint4*>(recp + (at < REC_HEAD / 16 ? 0 : SKIP))[at];
+            rec[j] = reinterpret_cast<const half8*>(recp + (at < REC_HEAD / 16 ? 0 : SKIP))[at];
         }
     }
 
@@ -411,12 +411,12 @@ struct Loader {
         }
 #pragma unroll
         for (int j = 0; j < RECP; ++j)
-            reinterpret_cast<uint4*>(buf + Lds::O_REC)[min(tid + NT * j, Lds::REC / 16 - 1)] = rec[j];
+            reinterpret_cast<half8*>(buf + Lds::O_REC)[min(tid + NT * j, Lds::REC / 16 - 1)] = rec[j];
 #pragma unroll
         for (int j = 0; j < VP; ++j) {
             const int i = (tid + NT * j) % (GC * VPR);
-            *reinterpret_cast<uint4*>(buf + Lds::O_V + i / VPR * Lds::V_ROW + 16 * (i % VPR)) =
-                keep_v ? v[j] : make_uint4(0, 0, 0, 0);
+            *reinterpret_cast<half8*>(buf + Lds::O_V + i / VPR * Lds::V_ROW + 16 * (i % VPR)) =
+                keep_v ? v[j] : half8{};
         }
     }
 };

@@ -39,15 +39,33 @@ __global__ __launch_bounds__(256) void gdr_prep_kernel(const ChunkArgs<T> a)
     const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, gq = lane >> 4, li = lane & 15;
     const int hk = h / a.rep;
 
-    // cumulative decays: lane = token, in every wave (the values of tokens past the end change nothing)
-    double l = 0.0;
-    float be = 0.f;
-    if (lane < len) {
-        const size_t at = (size_t)(c0 + lane) * a.H + h;
-        // a gate of 0 counts as 2^-100: what it lets through is lost against anything beside it
-        l = log2((double)fmaxf(to_f32(a.alpha[at]), 0x1p-100f));
-        be = to_f32(a.beta[at]);
-    }
+    // all loads on their way first: the gates, this wave's rows of K and Q, the blocks of K before them
+    const size_t gate_at = (size_t)(c0 + min(lane, len - 1)) * a.H + h;
+    const T gate = a.alpha[gate_at], strength = a.beta[gate_at];
+    const T* kbase = a.k + ((size_t)c0 * a.Hk + hk) * DK + gq * (Fr::KF / 4);
+    const T* qbase = a.q + ((size_t)c0 * a.Hk + hk) * DK + gq * (Fr::KF / 4);
+    const size_t step = (size_t)a.Hk * DK;
+    auto load_rows = [&](const T* base, int b, V* f) {
+        const T* p = base + min(16 * b + li, len - 1) * step;
+#pragma unroll
+        for (int s = 0; s < Fr::NS; ++s) f[s] = Fr::ld(p + s * Fr::KF);
+    };
+    auto cut_rows = [&](int b, V* f) {  // rows past the end count as 0
+        const bool in = 16 * b + li < len;
+#pragma unroll
+        for (int s = 0; s < Fr::NS; ++s)
+            if (!in) f[s] = V{};
+    };
+    V fk[Fr::NS], fq[Fr::NS], fc[3][Fr::NS];
+    load_rows(kbase, w, fk);
+    load_rows(qbase, w, fq);
+#pragma unroll
+    for (int c = 0; c < 3; ++c) load_rows(kbase, min(c, w), fc[c]);
+
+    // cumulative decays: lane = token, in every wave (the values of tokens past the end change nothing);
+    // a gate of 0 counts as 2^-100: what it lets through is lost against anything beside it
+    double l = lane < len ? log2((double)fmaxf(to_f32(gate), 0x1p-100f)) : 0.0;
+    const float be = lane < len ? to_f32(strength) : 0.f;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
         const double y = __shfl_up(l, off, 64);
@@ -59,21 +77,10 @@ __global__ __launch_bounds__(256) void gdr_prep_kernel(const ChunkArgs<T> a)
     }
     const double l_end = __shfl(l, 63, 64);
 
-    // operands: this wave's rows of K and Q
-    const T* kbase = a.k + ((size_t)c0 * a.Hk + hk) * DK + gq * (Fr::KF / 4);
-    const T* qbase = a.q + ((size_t)c0 * a.Hk + hk) * DK + gq * (Fr::KF / 4);
-    const size_t step = (size_t)a.Hk * DK;
-    auto load_rows = [&](const T* base, int b, V* f) {
-        const int t = 16 * b + li;
+    cut_rows(w, fk);
+    cut_rows(w, fq);
 #pragma unroll
-        for (int s = 0; s < Fr::NS; ++s) {
-            f[s] = V{};
-            if (t < len) f[s] = Fr::ld(base + t * step + s * Fr::KF);
-        }
-    };
-    V fk[Fr::NS], fq[Fr::NS];
-    load_rows(kbase, w, fk);
-    load_rows(qbase, w, fq);
+    for (int c = 0; c < 3; ++c) cut_rows(min(c, w), fc[c]);
     // power-of-two scales of the rows
     float mk = 0.f, mq = 0.f;
 #pragma unroll
@@ -96,6 +103,7 @@ __global__ __launch_bounds__(256) void gdr_prep_kernel(const ChunkArgs<T> a)
     double lr[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) lr[r] = s_l[16 * w + 4 * gq + r];
+#pragma unroll
     for (int c = 0; c < 4; ++c) {
         float* am = sM + 16 * c + li;
         if (c > w) {  // above the diagonal
@@ -103,13 +111,12 @@ __global__ __launch_bounds__(256) void gdr_prep_kernel(const ChunkArgs<T> a)
             for (int r = 0; r < 4; ++r) am[(16 * w + 4 * gq + r) * MP] = 0.f;
             continue;
         }
-        V fc[Fr::NS];
-        load_rows(kbase, c, fc);
         floatx4 kk = zero4(), qk = zero4();
 #pragma unroll
         for (int s = 0; s < Fr::NS; ++s) {
-            kk = Fr::mma(kk, fk[s], fc[s]);
-            qk = Fr::mma(qk, fq[s], fc[s]);
+            const V x = c < 3 ? fc[c < 3 ? c : 0][s] : fk[s];
+            kk = Fr::mma(kk, fk[s], x);
+            qk = Fr::mma(qk, fq[s], x);
         }
         const double ls = s_l[16 * c + li];
         float* lt = c == w ? sD[w] : sL[w * (w - 1) / 2 + c];
