@@ -7,7 +7,10 @@ namespace {
 
 using namespace kdn;
 
-kdn_status_t check_heads(int32_t H, int32_t Hk, int32_t dk, int32_t dv, kdn_dtype_t dtype,
+// Offsets within a chunk of 64 tokens have 32 bits; a grid at most 2^32 threads.
+bool heads_fit(int32_t N, int32_t H) { return H <= 65535 && (int64_t)N * H <= (1 << 20); }
+
+kdn_status_t check_heads(int32_t N, int32_t H, int32_t Hk, int32_t dk, int32_t dv, kdn_dtype_t dtype,
                          float scale)
 {
     if (dtype != KDN_F32 && dtype != KDN_BF16)
@@ -18,14 +21,20 @@ kdn_status_t check_heads(int32_t H, int32_t Hk, int32_t dk, int32_t dv, kdn_dtyp
         return fail(KDN_ERR_UNSUPPORTED, "dk=%d dv=%d: head sizes must be 16, 32, 64 or 128", dk,
                     dv);
     if (!(scale > 0.f)) return fail(KDN_ERR_INVALID_ARG, "scale must be positive (%g)", scale);
+    if (!heads_fit(N, H))
+        return fail(KDN_ERR_UNSUPPORTED, "%d sequences of H=%d: at most 65535 heads, and 2^20 in all", N,
+                    H);
     return KDN_OK;
 }
 
-// Rows of a few tokens go token by token.
-bool gdr_short(int32_t B, int32_t T)
+// Short rows go token by token: one launch in place of two, no chunk of 64 to fill. In us, token by
+// token against over chunks, bf16: 16 heads of d 128, one row of 8, 12, 16 tokens 11.7, 13.6, 17.4
+// against 16; 8 rows 11.7, 15.8, 19.6 (24 tokens: 27.1) against 22.5; 64 rows of 16, 32, 64 tokens 51,
+// 95, 184 against 108, 110, 113; 8 heads of d 64, 64 rows of 32 tokens 24 against 31. Packed rows, whose
+// lengths the host does not know, count as one.
+bool gdr_short(int32_t B, int32_t T, int32_t H)
 {
-    (void)B;
-    return T <= 8;
+    return T <= 12 || (T <= 32 && (int64_t)B * H >= 512);
 }
 
 }  // namespace
@@ -39,9 +48,9 @@ kdn_status_t kdn_decode_step_gdr(const void* q, const void* k, const void* v, co
 {
     if (!q || !k || !v || !alpha || !beta || !S || !o)
         return fail(KDN_ERR_INVALID_ARG, "null required pointer (q, k, v, alpha, beta, S, o)");
-    kdn_status_t st = check_heads(H, Hk, dk, dv, dtype, scale);
+    kdn_status_t st = check_heads(R, H, Hk, dk, dv, dtype, scale);
     if (st != KDN_OK) return st;
-    if (R < 0 || num_slots <= 0 || (int64_t)R * H > ((int64_t)1 << 31) / 128)
+    if (R < 0 || num_slots <= 0)
         return fail(KDN_ERR_INVALID_ARG, "bad sizes (R=%d num_slots=%d H=%d)", R, num_slots, H);
     if (!slot_idx && R > num_slots)
         return fail(KDN_ERR_INVALID_ARG, "without slot_idx R (%d) must not exceed num_slots (%d)",
@@ -64,8 +73,8 @@ kdn_status_t kdn_decode_step_gdr(const void* q, const void* k, const void* v, co
 size_t kdn_forward_gdr_workspace_bytes(int32_t N, int32_t B, int32_t T, int32_t H, int32_t Hk,
                                        int32_t dk, int32_t dv, kdn_dtype_t dtype, int32_t packed)
 {
-    if (N <= 0 || B <= 0 || T <= 0 || H <= 0 || Hk <= 0 || H % Hk != 0 || !head_ok(dk) ||
-        !head_ok(dv) || (dtype != KDN_F32 && dtype != KDN_BF16) || gdr_short(B, T))
+    if (N <= 0 || B <= 0 || T <= 0 || H <= 0 || Hk <= 0 || H % Hk != 0 || !heads_fit(N, H) ||
+        !head_ok(dk) || !head_ok(dv) || (dtype != KDN_F32 && dtype != KDN_BF16) || gdr_short(B, T, H))
         return 0;
     return gdr_chunk_workspace_bytes(packed != 0, N, B, T, H, dtype);
 }
@@ -78,7 +87,7 @@ kdn_status_t kdn_forward_gdr(const void* q, const void* k, const void* v, const 
 {
     if (!q || !k || !v || !alpha || !beta || !o)
         return fail(KDN_ERR_INVALID_ARG, "null required pointer (q, k, v, alpha, beta, o)");
-    kdn_status_t st = check_heads(H, Hk, dk, dv, dtype, scale);
+    kdn_status_t st = check_heads(N, H, Hk, dk, dv, dtype, scale);
     if (st == KDN_OK) st = check_seq(cu_seqlens, N, B, T, H);
     if (st == KDN_OK)
         st = check_aligned({{q, "q"}, {k, "k"}, {v, "v"}, {o, "o"}, {S0, "S0"}, {S_T, "S_T"}});
@@ -106,7 +115,7 @@ kdn_status_t kdn_forward_gdr(const void* q, const void* k, const void* v, const 
         return fail(KDN_ERR_INVALID_ARG, "the workspace overlaps an output");
     const GdrCall c = {q, k, v, alpha, beta, S0, o, S_T, {cu_seqlens, N, B, T, H}, Hk, dk, dv,
                        dtype, scale, workspace};
-    return hip_status(gdr_short(B, T) ? launch_gdr_recurrent(c, (hipStream_t)stream)
+    return hip_status(gdr_short(B, T, H) ? launch_gdr_recurrent(c, (hipStream_t)stream)
                                       : launch_gdr_chunked(c, (hipStream_t)stream),
                       "kdn_forward_gdr launch");
 }
@@ -114,8 +123,8 @@ kdn_status_t kdn_forward_gdr(const void* q, const void* k, const void* v, const 
 size_t kdn_backward_gdr_workspace_bytes(int32_t N, int32_t B, int32_t T, int32_t H, int32_t Hk,
                                         int32_t dk, int32_t dv, kdn_dtype_t dtype, int32_t packed)
 {
-    if (N <= 0 || B <= 0 || T <= 0 || H <= 0 || Hk <= 0 || H % Hk != 0 || !head_ok(dk) ||
-        !head_ok(dv) || (dtype != KDN_F32 && dtype != KDN_BF16))
+    if (N <= 0 || B <= 0 || T <= 0 || H <= 0 || Hk <= 0 || H % Hk != 0 || !heads_fit(N, H) ||
+        !head_ok(dk) || !head_ok(dv) || (dtype != KDN_F32 && dtype != KDN_BF16))
         return 0;
     return gdr_backward_workspace_bytes(packed != 0, N, B, T, H, dk, dv, dtype);
 }
@@ -131,7 +140,7 @@ kdn_status_t kdn_backward_gdr(const void* q, const void* k, const void* v, const
         return fail(KDN_ERR_INVALID_ARG, "null required input (q, k, v, alpha, beta)");
     if (!dq || !dk_out || !dv_out || !dalpha || !dbeta)
         return fail(KDN_ERR_INVALID_ARG, "null required gradient (dq, dk, dv, dalpha, dbeta)");
-    kdn_status_t st = check_heads(H, Hk, dk, dv, dtype, scale);
+    kdn_status_t st = check_heads(N, H, Hk, dk, dv, dtype, scale);
     if (st == KDN_OK) st = check_seq(cu_seqlens, N, B, T, H);
     if (st == KDN_OK)
         st = check_aligned({{q, "q"}, {k, "k"}, {v, "v"}, {dO, "dO"}, {S0, "S0"}, {dS_T, "dS_T"},

@@ -275,3 +275,30 @@ def test_refusals():
         kdn.backward_gdr(q, k, v, a, b, dS_T=torch.zeros(1, 2, 32, 32, device="cuda").bfloat16())
     with pytest.raises(ValueError):
         kdn.decode_step_gdr(q[0], k[0], v[0], a[0], b[0], torch.zeros(9, 1, 32, 32, device="cuda"))
+
+
+def test_too_many_heads():
+    """32-bit offsets within a chunk and the grid bound the heads of a call."""
+    H = 65552
+    z = [torch.zeros(1, 9, n, 16, dtype=torch.bfloat16, device="cuda") for n in (16, 16, H)]
+    g = torch.zeros(1, 9, H, dtype=torch.bfloat16, device="cuda")
+    for f in (kdn.forward_gdr, kdn.backward_gdr):
+        with pytest.raises(kdn.KdnError):
+            f(*z, g, g)
+    R = (1 << 20) // 16 + 1  # rows of 16 heads
+    z = [torch.zeros(R, 1, 16, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    v = torch.zeros(R, 16, 16, dtype=torch.bfloat16, device="cuda")
+    g = torch.zeros(R, 16, dtype=torch.bfloat16, device="cuda")
+    slots = torch.zeros(R, dtype=torch.int32, device="cuda")
+    with pytest.raises(kdn.KdnError):
+        kdn.decode_step_gdr(*z, v, g, g, torch.zeros(1, 16, 16, 16, device="cuda"), slots)
+
+
+@pytest.mark.parametrize("B,T,H", [(1, 12, 2), (1, 13, 2), (64, 32, 8), (64, 33, 8), (63, 32, 8)])
+def test_either_side_of_the_short_rows(B, T, H):
+    """The forms that run token by token and over chunks, where one takes over from the other."""
+    x = R.draw(T, B, T, H, H, 16, 32, state=True)
+    d = dev(x, "f32")
+    o, S = kdn.forward_gdr(*[d[n] for n in NAMES], S0=d["S0"])
+    want_o, want_S = R.forward(x)
+    assert near(o, want_o, "f32") and near(S, want_S, "f32")
