@@ -1,0 +1,151 @@
+"""A small language model on the gated delta rule, trained and then decoded with beam search: the
+library's operators together as a program uses them.
+
+    python -m paper_2609_07816_amd.gdr_lm            # train on repeated random strings, continue some
+
+One mixer layer. The memory is written with the token before as key and the token itself as value and
+read with the token as query, so that it answers what followed the token earlier: enough to continue a
+string that repeats. Training runs forward_gdr and backward_gdr over whole sequences; serving runs the
+prompts, packed, through forward_gdr, puts their states into a slot pool, and then per token
+decode_step_gdr on every beam, beam_select on the logits and beam_reorder on the pool.
+"""
+
+import argparse
+
+import torch
+import torch.nn.functional as F
+
+from . import kdn
+
+
+class GatedDelta(torch.autograd.Function):
+    """kdn.forward_gdr with its gradients."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, alpha, beta):
+        o, _ = kdn.forward_gdr(q, k, v, alpha, beta)
+        ctx.save_for_backward(q, k, v, alpha, beta)
+        return o
+
+    @staticmethod
+    def backward(ctx, dO):
+        g = kdn.backward_gdr(*ctx.saved_tensors, dO=dO.contiguous())
+        return g["dq"], g["dk"], g["dv"], g["dalpha"], g["dbeta"]
+
+
+class GdrLM(torch.nn.Module):
+    """Embedding, one gated-delta mixer of H value heads on Hk key heads, output head."""
+
+    def __init__(self, vocab=64, width=64, heads=4, key_heads=2, dk=32, dv=32, dtype=torch.float32):
+        super().__init__()
+        self.H, self.Hk, self.dk, self.dv, self.dtype = heads, key_heads, dk, dv, dtype
+        self.embed = torch.nn.Embedding(vocab, width)
+        self.to_q = torch.nn.Linear(width, key_heads * dk, bias=False)
+        self.to_k = torch.nn.Linear(width, key_heads * dk, bias=False)
+        self.to_v = torch.nn.Linear(width, heads * dv, bias=False)
+        self.to_gates = torch.nn.Linear(width, 2 * heads)
+        self.head = torch.nn.Linear(heads * dv, vocab)
+        with torch.no_grad():  # keep what is written, write in full
+            self.to_gates.bias.fill_(4.0)
+
+    def inputs(self, token, before):
+        """The mixer's inputs for tokens [..] that follow the tokens `before` [..]."""
+        x, y = self.embed(token), self.embed(before)
+        lead = token.shape
+        q = F.normalize(self.to_q(x).view(*lead, self.Hk, self.dk), dim=-1)
+        k = F.normalize(self.to_k(y).view(*lead, self.Hk, self.dk), dim=-1)
+        v = self.to_v(x).view(*lead, self.H, self.dv)
+        gates = torch.sigmoid(self.to_gates(x))
+        alpha, beta = gates[..., :self.H], gates[..., self.H:]
+        return [t.to(self.dtype).contiguous() for t in (q, k, v, alpha, beta)]
+
+    def logits(self, o):
+        return self.head(o.flatten(-2).float())
+
+    def forward(self, tokens):
+        """Logits [B, T, vocab] of tokens [B, T]; the token before the first is 0."""
+        return self.logits(GatedDelta.apply(*self.inputs(tokens, F.pad(tokens[:, :-1], (1, 0)))))
+
+    @torch.no_grad()
+    def beam_search(self, prompts, steps, beams, end_token=0):
+        """Continues prompts (a list of 1-D token tensors) by up to `steps` tokens. Returns (tokens
+        [N, beams, steps], end_token after the end, scores [N, beams]), best first."""
+        dev, N = self.head.weight.device, len(prompts)
+        lens = torch.tensor([p.numel() for p in prompts])
+        cu = F.pad(lens.cumsum(0), (1, 0)).to(torch.int32)
+        token = torch.cat(prompts).to(dev)
+        before = torch.cat([F.pad(p[:-1], (1, 0)) for p in prompts]).to(dev)
+        o, S_T = kdn.forward_gdr(*self.inputs(token[None], before[None]), cu_seqlens=cu.to(dev))
+        ends = (cu[1:] - 1).to(dev).long()
+        # a slot for each beam, the prompt's state in that of the first; the others count from the
+        # first selection on, which forks them off it
+        pool = torch.zeros(N * beams, self.H, self.dk, self.dv, device=dev)
+        slots = torch.arange(N * beams, dtype=torch.int32, device=dev).view(N, beams)
+        pool[slots[:, 0].long()] = S_T
+        scores = torch.full((N, beams), -torch.inf, device=dev)
+        scores[:, 0] = 0.0
+        done = torch.zeros(N, beams, dtype=torch.bool, device=dev)
+        logits = self.logits(o[0, ends])[:, None].expand(N, beams, -1).contiguous()
+        last = token[ends][:, None].expand(N, beams).contiguous()
+        trail = []
+        for step in range(steps):
+            scores, new, parent, done = kdn.beam_select(logits, scores, done=done, end_token=end_token)
+            slots = kdn.beam_reorder(parent, slots, pool)
+            trail.append((new, parent))
+            if step + 1 == steps:
+                break
+            last, before = new.long(), last.gather(1, parent.long())
+            o = kdn.decode_step_gdr(*self.inputs(last.flatten(), before.flatten()), pool,
+                                    slot_idx=slots.flatten())
+            logits = self.logits(o).view(N, beams, -1)
+        at = torch.arange(beams, device=dev).expand(N, beams)
+        out = []
+        for new, parent in reversed(trail):
+            out.append(new.gather(1, at))
+            at = parent.long().gather(1, at)
+        return torch.stack(out[::-1], -1), scores
+
+
+def repeated(count, length, period, vocab, generator):
+    """Random strings of `period` distinct tokens (none of them 0), repeated up to `length`."""
+    once = torch.stack([torch.randperm(vocab - 1, generator=generator)[:period] + 1
+                        for _ in range(count)])
+    return once.repeat(1, -(-length // period))[:, :length]
+
+
+def train(model, steps, generator, batch=16, length=97, period=20, lr=1e-2):
+    """Adam on repeated strings; returns every step's loss over the tokens after the first period."""
+    dev, vocab = model.head.weight.device, model.head.out_features
+    opt, losses = torch.optim.Adam(model.parameters(), lr=lr), []
+    for _ in range(steps):
+        x = repeated(batch, length, period, vocab, generator).to(dev)
+        y = model(x[:, :-1])[:, period:]
+        loss = F.cross_entropy(y.flatten(0, 1), x[:, period + 1:].flatten())
+        opt.zero_grad()
+        loss.backward()
+        opt.step()
+        losses.append(loss.detach())
+    return torch.stack(losses).cpu()
+
+
+def main():
+    p = argparse.ArgumentParser(description=__doc__.splitlines()[0])
+    p.add_argument("--steps", type=int, default=150, help="training steps")
+    p.add_argument("--beams", type=int, default=4)
+    p.add_argument("--dtype", choices=["bf16", "f32"], default="bf16", help="of the mixer")
+    args = p.parse_args()
+    torch.manual_seed(0)
+    gen = torch.Generator().manual_seed(0)
+    model = GdrLM(dtype=torch.bfloat16 if args.dtype == "bf16" else torch.float32).cuda()
+    losses = train(model, args.steps, gen)
+    print(f"loss {losses[0]:.3f} -> {losses[-1]:.3f} nats per token")
+    full = repeated(4, 80, 20, 64, gen)
+    cut = (30, 41, 47, 60)
+    tokens, scores = model.beam_search([x[:n] for x, n in zip(full, cut)], 20, args.beams)
+    for x, n, best, score in zip(full, cut, tokens[:, 0].cpu(), scores[:, 0].tolist()):
+        right = int((best == x[n:n + 20]).sum())
+        print(f"prompt of {n}: {right} of 20 tokens continue the string, log-probability {score:.2f}")
+
+
+if __name__ == "__main__":
+    main()
