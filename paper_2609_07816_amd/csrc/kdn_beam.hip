@@ -5,9 +5,10 @@
 // with x the beam's logits and m the largest. Within a beam the order of scores is the order of
 // logits, so nothing needs the sum before the end, and one pass reads the logits: each wavefront takes
 // a piece of a row, keeps the running maximum and sum of its exponentials per lane, and the W largest
-// logits in order, one per lane (entry i in lane i). A tile of 512 values enters that list only by
-// values above its W-th entry: a round takes the tile's largest, and rounds end once that is not
-// above it. The second kernel joins a row's pieces (lane = piece, each round takes the best head), then
+// logits in order, one per lane (entry i in lane i). Of a tile of 512 values only those above the W-th
+// entry enter that list, one after another in order of tokens (taking the tile's largest first, round
+// by round, cost five times the instructions per value: 34 us in place of PIECE_US at 384 rows of
+// 50,021). The second kernel joins a row's pieces (lane = piece, each round takes the best head), then
 // the rows (lane = beam). Values are compared as integers in the same order as the floats; 0 is below
 // every value and marks places without one. The sums are float32 in a fixed order: no atomics.
 #include "kdn_beam.h"
@@ -59,30 +60,34 @@ struct Entry {
     unsigned key, token;
 };
 
-// Eight values of a row from place `at`, in one load whatever the row's alignment (rows of odd length
-// start anywhere; global loads need none): the places of a lane, and so the order of the sums, depend
-// on the row alone. Places past the row's end are not read.
 template <class T>
-__device__ __forceinline__ void load8(const T* row, int V, int at, float* x, bool* in)
-{
-    struct __attribute__((packed, aligned(sizeof(T)))) V8 { T v[8]; };
-    if (at + 8 <= V) {
-        const V8 y = *reinterpret_cast<const V8*>(row + at);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            x[e] = to_f32(y.v[e]);
-            in[e] = true;
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            in[e] = at + e < V;
-            x[e] = in[e] ? to_f32(row[at + e]) : 0.f;
-        }
+struct __attribute__((packed, aligned(sizeof(T)))) Values8 {
+    T v[8];
+};
+
+// The list of a wavefront: entry i in lane i, in order of the keys, equal ones of the lowest token first.
+struct List {
+    unsigned key = 0, token = 0;
+
+    // A value that comes after the others in order of tokens; returns the W-th key.
+    __device__ __forceinline__ unsigned insert(unsigned k, unsigned tok, int lane, int W)
+    {
+        const int pos = __builtin_popcountll(__ballot(key >= k));  // sorted: a prefix
+        const unsigned pk = lane_before(key), pt = lane_before(token);
+        key = lane > pos ? pk : lane == pos ? k : key;
+        token = lane > pos ? pt : lane == pos ? tok : token;
+        if (lane >= W) key = 0;
+        return (unsigned)__builtin_amdgcn_readlane((int)key, W - 1);
     }
-}
+    __device__ static __forceinline__ unsigned lane_before(unsigned x)  // wave_shr 1
+    {
+        return (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x138, 0xf, 0xf, false);
+    }
+};
 
 // Grid: (pieces of a row, rows), 64 threads. stats [rows][pieces] (m, sum), best [rows][pieces][W].
+// Bound by its own instructions (a wavefront per piece, all of them resident at once), not by the 8 us
+// that the logits take at the copy rate: 384 rows (a fifth of them finished) of 50,021 bf16 logits, W 8.
 template <class T>
 __global__ __launch_bounds__(64) void beam_piece_kernel(const T* __restrict__ logits,
                                                         const uint8_t* __restrict__ done, int W,
@@ -94,56 +99,66 @@ __global__ __launch_bounds__(64) void beam_piece_kernel(const T* __restrict__ lo
     if (done && done[row]) return;
     const T* x0 = logits + row * (size_t)V;
     const int first = piece * tiles * TILE;
-    unsigned lkey = 0, ltok = 0, thr = 0;  // this lane's entry of the list, and its W-th key
+    List list;
+    unsigned thr = 0;  // what a value has to exceed to enter
     float m = -INFINITY, s = 0.f;
+    // Eight values of a lane in one load whatever the row's alignment (rows of odd length start anywhere;
+    // global loads need none): the places of a lane, and so the order of the sums, depend on the row
+    // alone. The next tile is on its way while this one is worked on; places past the row's end are not
+    // read.
+    auto fetch = [&](int at) {
+        Values8<T> y = {};
+        if (at + 8 <= V) y = *reinterpret_cast<const Values8<T>*>(x0 + at);
+        return y;
+    };
+    Values8<T> next = fetch(first + 8 * lane);
     for (int t = 0; t < tiles; ++t) {
-        const int at = first + t * TILE + 8 * lane;
-        if (first + t * TILE >= V) break;
+        const int base = first + t * TILE, at = base + 8 * lane;
+        if (base >= V) break;
+        Values8<T> y = next;
+        if (t + 1 < tiles) next = fetch(at + TILE);
+        const bool whole = base + TILE <= V;  // uniform
+        if (!whole && at + 8 > V)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (at + e < V) y.v[e] = x0[at + e];
         float x[8];
-        bool in[8];
-        load8(x0, V, at, x, in);
-        unsigned key[8];
+        unsigned key[8], b = 0;
         float mt = m;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            key[e] = in[e] ? order_key(x[e]) : 0u;
-            x[e] = in[e] ? key_value(key[e]) : -INFINITY;
+            key[e] = order_key(to_f32(y.v[e]));
+            if (!whole && at + e >= V) key[e] = 0;
+            x[e] = key[e] ? key_value(key[e]) : -INFINITY;
             mt = fmaxf(mt, x[e]);
+            b = max(b, key[e]);
         }
         const float ref = mt == -INFINITY ? 0.f : mt;
         s *= exp_diff(m, ref);
 #pragma unroll
         for (int e = 0; e < 8; ++e) s += exp_diff(x[e], ref);
         m = mt;
-        for (;;) {
-            unsigned b = key[0];
-            int be = 0;
-#pragma unroll
-            for (int e = 1; e < 8; ++e)
-                if (key[e] > b) {
-                    b = key[e];
-                    be = e;
-                }
-            const unsigned mx = wave_umax(b);
-            if (mx <= thr) break;
-            // the lowest lane of an equal value has the lowest token
-            const int win = __builtin_ctzll(__ballot(b == mx));
-            const unsigned tok = (unsigned)__builtin_amdgcn_readlane(at + be, win);
-            if (lane == win)
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (e == be) key[e] = 0;
-            const int pos = __builtin_popcountll(__ballot(lkey >= mx));  // sorted: a prefix
-            const unsigned pk = __shfl_up(lkey, 1), pt = __shfl_up(ltok, 1);
-            if (lane > pos) {
-                lkey = pk;
-                ltok = pt;
-            } else if (lane == pos) {
-                lkey = mx;
-                ltok = tok;
+        if (t == 0) {
+            // the W-th of the lanes' largest: at least W values are no less, so none below it enters
+            unsigned c = b, w_th = 0;
+            for (int i = 0; i < W; ++i) {
+                w_th = wave_umax(c);
+                if (lane == __builtin_ctzll(__ballot(c == w_th))) c = 0;
             }
-            if (lane >= W) lkey = 0;
-            thr = (unsigned)__builtin_amdgcn_readlane((int)lkey, W - 1);
+            thr = w_th ? w_th - 1 : 0;
+        }
+        // lane by lane, in order of tokens, so that an equal value never precedes an entry
+        unsigned long long todo = ~0ull;
+        for (;;) {
+            const unsigned long long in = __ballot(b > thr) & todo;
+            if (!in) break;
+            const int l = __builtin_ctzll(in);
+            todo = l == 63 ? 0 : ~0ull << (l + 1);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const unsigned k = (unsigned)__builtin_amdgcn_readlane((int)key[e], l);
+                if (k > thr) thr = max(thr, list.insert(k, (unsigned)(base + 8 * l + e), lane, W));
+            }
         }
     }
     const float M = key_value(wave_umax(order_key(m)));
@@ -151,7 +166,7 @@ __global__ __launch_bounds__(64) void beam_piece_kernel(const T* __restrict__ lo
     const float sum = wave_sum(s * exp_diff(m, ref));
     const size_t o = row * pieces + piece;
     if (lane == 0) stats[o] = make_float2(M, sum);
-    if (lane < W) best[o * W + lane] = Entry{lkey, ltok};
+    if (lane < W) best[o * W + lane] = Entry{list.key, list.token};
 }
 
 // Grid: batch elements; `blockDim.x / 64` wavefronts take its rows in turn. Dynamic LDS: the rows'
@@ -235,20 +250,20 @@ __global__ void beam_join_kernel(const float* __restrict__ scores, const uint8_t
 // everything in place, and only what a fork needs: 2 bytes moved per byte forked. Every workgroup
 // finds its child's slots from its batch element's W parents.
 // ------------------------------------------------------------------------------------------
-constexpr int COPY_UNROLL = 8;
-constexpr size_t COPY_PIECE = 256 * 16 * COPY_UNROLL;  // bytes of a workgroup: 32 KB
+constexpr int COPY_UNROLL = 4;
+constexpr size_t COPY_PIECE = 256 * 16 * COPY_UNROLL;  // bytes of a workgroup: 16 KB
 
 __device__ __forceinline__ void copy_piece(const char* src, char* dst, size_t bytes)
 {
     const int tid = threadIdx.x;
     if ((((uintptr_t)src | (uintptr_t)dst | bytes) & 15) == 0) {
-        const uint4* s = reinterpret_cast<const uint4*>(src);
-        uint4* d = reinterpret_cast<uint4*>(dst);
+        typedef unsigned u4 __attribute__((ext_vector_type(4)));
+        const u4* s = reinterpret_cast<const u4*>(src);
+        u4* d = reinterpret_cast<u4*>(dst);
         const int n = (int)(bytes / 16);
-        uint4 x[COPY_UNROLL];
+        u4 x[COPY_UNROLL];
 #pragma unroll
-        for (int i = 0; i < COPY_UNROLL; ++i)
-            if (tid + 256 * i < n) x[i] = s[tid + 256 * i];
+        for (int i = 0; i < COPY_UNROLL; ++i) x[i] = s[min(tid + 256 * i, n - 1)];
 #pragma unroll
         for (int i = 0; i < COPY_UNROLL; ++i)
             if (tid + 256 * i < n) d[tid + 256 * i] = x[i];
