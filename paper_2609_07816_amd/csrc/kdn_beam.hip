@@ -6,9 +6,8 @@
 // logits, so nothing needs the sum before the end, and one pass reads the logits: each wavefront takes
 // a piece of a row, keeps the running maximum and sum of its exponentials per lane, and the W largest
 // logits in order, one per lane (entry i in lane i). Of a tile of 512 values only those above the W-th
-// entry enter that list, one after another in order of tokens (taking the tile's largest first, round
-// by round, cost five times the instructions per value: 34 us in place of PIECE_US at 384 rows of
-// 50,021). The second kernel joins a row's pieces (lane = piece, each round takes the best head), then
+// entry enter that list, one after another (taking the tile's largest first, round by round, took 34 us
+// in place of 30 at 384 rows of 50,021; reading off the candidates lane by lane 49). The second kernel joins a row's pieces (lane = piece, each round takes the best head), then
 // the rows (lane = beam). Values are compared as integers in the same order as the floats; 0 is below
 // every value and marks places without one. The sums are float32 in a fixed order: no atomics.
 #include "kdn_beam.h"
@@ -22,13 +21,16 @@ constexpr int MAX_PIECES = 64;  // pieces of a row: one lane each when they are 
 
 // floats as integers of the same order; a NaN counts as -inf, +inf as the largest finite value and
 // -0 as 0
-__device__ __forceinline__ unsigned order_key(float x)
+__device__ __forceinline__ float counted(float x)
 {
-    if (!(x == x)) x = -INFINITY;
-    x = fminf(x, 3.402823466e38f) + 0.f;
-    const unsigned u = __float_as_uint(x);
-    return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+    return fminf(fmaxf(x, -INFINITY), 3.402823466e38f);
 }
+__device__ __forceinline__ unsigned bits_key(unsigned u)  // of a counted value's bits
+{
+    u = u == 0x80000000u ? 0u : u;
+    return u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ unsigned order_key(float x) { return bits_key(__float_as_uint(counted(x))); }
 __device__ __forceinline__ float key_value(unsigned k)
 {
     return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k);
@@ -65,19 +67,25 @@ struct __attribute__((packed, aligned(sizeof(T)))) Values8 {
     T v[8];
 };
 
-// The list of a wavefront: entry i in lane i, in order of the keys, equal ones of the lowest token first.
+// The list of a wavefront: entry i in lane i, in order of the keys, equal ones of the lowest token first;
+// its W-th entry (uniform).
 struct List {
-    unsigned key = 0, token = 0;
+    unsigned key = 0, token = 0, last_key = 0, last_token = 0;
 
-    // A value that comes after the others in order of tokens; returns the W-th key.
-    __device__ __forceinline__ unsigned insert(unsigned k, unsigned tok, int lane, int W)
+    __device__ __forceinline__ void insert(unsigned k, unsigned tok, int lane, int W)
     {
-        const int pos = __builtin_popcountll(__ballot(key >= k));  // sorted: a prefix
+        const unsigned long long above = __ballot(key > k), same = __ballot(key == k),
+                                 lower = __ballot(token < tok);
+        const int pos = __builtin_popcountll(above | (same & lower));  // sorted: a prefix
         const unsigned pk = lane_before(key), pt = lane_before(token);
         key = lane > pos ? pk : lane == pos ? k : key;
         token = lane > pos ? pt : lane == pos ? tok : token;
         if (lane >= W) key = 0;
-        return (unsigned)__builtin_amdgcn_readlane((int)key, W - 1);
+        const unsigned lk = (unsigned)__builtin_amdgcn_readlane((int)key, W - 1);
+        if (lk >= last_key && lk) {
+            last_key = lk;
+            last_token = (unsigned)__builtin_amdgcn_readlane((int)token, W - 1);
+        }
     }
     __device__ static __forceinline__ unsigned lane_before(unsigned x)  // wave_shr 1
     {
@@ -86,8 +94,10 @@ struct List {
 };
 
 // Grid: (pieces of a row, rows), 64 threads. stats [rows][pieces] (m, sum), best [rows][pieces][W].
-// Bound by its own instructions (a wavefront per piece, all of them resident at once), not by the 8 us
-// that the logits take at the copy rate: 384 rows (a fifth of them finished) of 50,021 bf16 logits, W 8.
+// Bound by its own instructions, some 30 per value and wavefront (the exponential, the order of keys, the
+// list), with every wavefront resident at once: 384 rows (a fifth of them finished) of 50,021 bf16 logits,
+// W 8, take 30 us, 80 rows of 131,072 float32 ones, W 5, 19 us; reading them alone 6 and 8.5 us at the copy
+// rate. Half and a quarter as many pieces measured the same and slower.
 template <class T>
 __global__ __launch_bounds__(64) void beam_piece_kernel(const T* __restrict__ logits,
                                                         const uint8_t* __restrict__ done, int W,
@@ -100,7 +110,6 @@ __global__ __launch_bounds__(64) void beam_piece_kernel(const T* __restrict__ lo
     const T* x0 = logits + row * (size_t)V;
     const int first = piece * tiles * TILE;
     List list;
-    unsigned thr = 0;  // what a value has to exceed to enter
     float m = -INFINITY, s = 0.f;
     // Eight values of a lane in one load whatever the row's alignment (rows of odd length start anywhere;
     // global loads need none): the places of a lane, and so the order of the sums, depend on the row
@@ -127,9 +136,10 @@ __global__ __launch_bounds__(64) void beam_piece_kernel(const T* __restrict__ lo
         float mt = m;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            key[e] = order_key(to_f32(y.v[e]));
+            x[e] = counted(to_f32(y.v[e]));
+            if (!whole && at + e >= V) x[e] = -INFINITY;
+            key[e] = bits_key(__float_as_uint(x[e]));
             if (!whole && at + e >= V) key[e] = 0;
-            x[e] = key[e] ? key_value(key[e]) : -INFINITY;
             mt = fmaxf(mt, x[e]);
             b = max(b, key[e]);
         }
@@ -145,19 +155,23 @@ __global__ __launch_bounds__(64) void beam_piece_kernel(const T* __restrict__ lo
                 w_th = wave_umax(c);
                 if (lane == __builtin_ctzll(__ballot(c == w_th))) c = 0;
             }
-            thr = w_th ? w_th - 1 : 0;
+            list.last_key = w_th ? w_th - 1 : 0;
         }
-        // lane by lane, in order of tokens, so that an equal value never precedes an entry
-        unsigned long long todo = ~0ull;
-        for (;;) {
-            const unsigned long long in = __ballot(b > thr) & todo;
-            if (!in) break;
-            const int l = __builtin_ctzll(in);
-            todo = l == 63 ? 0 : ~0ull << (l + 1);
+        if (!__ballot(b > list.last_key)) continue;  // later tiles have higher tokens: no ties enter
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const unsigned k = (unsigned)__builtin_amdgcn_readlane((int)key[e], l);
-                if (k > thr) thr = max(thr, list.insert(k, (unsigned)(base + 8 * l + e), lane, W));
+        for (int e = 0; e < 8; ++e) {
+            // not in order of tokens: among equal values the lowest token counts
+            unsigned long long todo = ~0ull;
+            for (;;) {
+                const unsigned long long in =
+                    (__ballot(key[e] > list.last_key) |
+                     (__ballot(key[e] == list.last_key) & __ballot((unsigned)(at + e) < list.last_token))) &
+                    todo;
+                if (!in) break;
+                const int l = __builtin_ctzll(in);
+                todo = l == 63 ? 0 : ~0ull << (l + 1);
+                list.insert((unsigned)__builtin_amdgcn_readlane((int)key[e], l),
+                            (unsigned)(base + 8 * l + e), lane, W);
             }
         }
     }
@@ -250,6 +264,9 @@ __global__ void beam_join_kernel(const float* __restrict__ scores, const uint8_t
 // everything in place, and only what a fork needs: 2 bytes moved per byte forked. Every workgroup
 // finds its child's slots from its batch element's W parents.
 // ------------------------------------------------------------------------------------------
+// Bound by memory: 240 forked states of 1 MB (500 MB moved) in 60 to 75 us, which the cache behind the L2s
+// helps, 57 of them (120 MB) in 20 us. 16 KB a workgroup, all its loads in flight in registers: 32 KB
+// measured the same, 8 KB 25 us more.
 constexpr int COPY_UNROLL = 4;
 constexpr size_t COPY_PIECE = 256 * 16 * COPY_UNROLL;  // bytes of a workgroup: 16 KB
 
