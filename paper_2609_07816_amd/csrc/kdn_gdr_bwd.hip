@@ -33,17 +33,19 @@ struct GradArgs {
 // ------------------------------------------------------------------------------------------
 // gdr_reverse: as gdr_walk, the chunks in reverse and dS in registers.
 // ------------------------------------------------------------------------------------------
+template <class T, int DK, int NCW>
+using ReverseLds = ChunkLds<T, DK, true, 4, 16 * NCW>;
+
 template <class T, int DK, int DV, int NCW, int NLW>
-__global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_reverse_kernel(const GradArgs<T> ga)
+__device__ __forceinline__ void gdr_reverse(const GradArgs<T>& ga, int block, char* lds)
 {
-    using Sh = ChunkLds<T, DK, true, 4, 16 * NCW>;
+    using Sh = ReverseLds<T, DK, NCW>;
     constexpr int P = Sh::P, KS = Sh::KSTEPS, KT = Sh::KT;
     const ChunkArgs<T>& a = ga.c;
     constexpr int REC = gdr_rec_bytes<T, true>();
     constexpr int TILES = DV / (16 * NCW);
-    __shared__ __align__(16) char lds[Sh::NBUF * Sh::BYTES];
     const int chains = a.seq.N * a.H;
-    const int chain = blockIdx.x / (8 * TILES) * 8 + blockIdx.x % 8, tile = blockIdx.x / 8 % TILES;
+    const int chain = block / (8 * TILES) * 8 + block % 8, tile = block / 8 % TILES;
     if (chain >= chains) return;
     const int n = chain / a.H, h = chain % a.H, hk = h / a.rep;
     int t0, t1;
@@ -349,6 +351,29 @@ __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_reverse_kernel(const Gra
         for (int k = 0; k < KT; ++k)
 #pragma unroll
             for (int r = 0; r < 4; ++r) ga.dS0[sbase + (size_t)(16 * k + r) * DV] = dS[k][r] * sS.i;
+}
+
+template <class T, int DK, int DV, int NCW, int NLW>
+__global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_reverse_kernel(const GradArgs<T> ga)
+{
+    using Sh = ReverseLds<T, DK, NCW>;
+    __shared__ __align__(16) char lds[Sh::NBUF * Sh::BYTES];
+    gdr_reverse<T, DK, DV, NCW, NLW>(ga, blockIdx.x, lds);
+}
+
+// Both walks in one launch, the longer one's workgroups first: neither reads what the other writes.
+template <class T, int DK, int DV, int NCW, int NLW>
+__global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_walks_kernel(const GradArgs<T> ga)
+{
+    using Rs = ReverseLds<T, DK, NCW>;
+    using Fs = WalkLds<T, DK, NCW, true>;
+    constexpr int RB = Rs::NBUF * Rs::BYTES, FB = Fs::NBUF * Fs::BYTES;
+    __shared__ __align__(16) char lds[RB > FB ? RB : FB];
+    const int half = gridDim.x / 2;
+    if ((int)blockIdx.x < half)
+        gdr_reverse<T, DK, DV, NCW, NLW>(ga, blockIdx.x, lds);
+    else
+        gdr_walk<T, DK, DV, NCW, NLW, true>(ga.c, ga.keep, blockIdx.x - half, lds);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -947,11 +972,18 @@ template <class T, int DK, int DV, int NCW, int NLW>
 hipError_t launch_rest(const GradArgs<T>& ga, hipStream_t stream)
 {
     const ChunkArgs<T>& a = ga.c;
-    constexpr int TILES = DV / (16 * NCW);
-    const unsigned grid = (unsigned)((a.seq.N * a.H + 7) / 8 * 8 * TILES);
-    hipLaunchKernelGGL((gdr_reverse_kernel<T, DK, DV, NCW, NLW>), dim3(grid), dim3(64 * (NCW + NLW)), 0,
-                       stream, ga);
-    const hipError_t e = hipGetLastError();
+    const unsigned grid = walk_grid<DV, NCW>(a.seq, a.H);
+    hipError_t e;
+    if (grid < 256) {
+        hipLaunchKernelGGL((gdr_walks_kernel<T, DK, DV, NCW, NLW>), dim3(2 * grid), dim3(64 * (NCW + NLW)),
+                           0, stream, ga);
+    } else {
+        e = launch_gdr_walk<true, T, DK, DV, NCW, NLW>(a, ga.keep, stream);
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL((gdr_reverse_kernel<T, DK, DV, NCW, NLW>), dim3(grid), dim3(64 * (NCW + NLW)), 0,
+                           stream, ga);
+    }
+    e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((gdr_grad_kernel<T, DK, DV>), dim3((unsigned)(a.maxch * a.Hk)), dim3(256), 0,
                        stream, ga);
@@ -1006,7 +1038,6 @@ hipError_t launch_t(const GdrGradCall& b, hipStream_t stream)
     const GradArgs<T> ga = {a, (const T*)b.dO, b.dS_T, (T*)b.dq, (T*)b.dk, (T*)b.dv, (T*)b.dalpha,
                             (T*)b.dbeta, b.dS0, keep};
     hipError_t e = launch_gdr_prep(a, c.dk, true, stream);
-    if (e == hipSuccess) e = launch_gdr_walk_dk<true>(a, keep, c.dk, c.dv, stream);
     if (e != hipSuccess) return e;
     switch (c.dk) {
     case 16: return launch_dv<T, 16>(ga, c.dv, stream);

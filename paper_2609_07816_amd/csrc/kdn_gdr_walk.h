@@ -78,17 +78,15 @@ template <class T, int DK, int NCW, bool BWD>
 using WalkLds = ChunkLds<T, DK, !BWD, BWD ? 2 : 2 + gdr_parts<T>(), 16 * NCW>;
 
 template <class T, int DK, int DV, int NCW, int NLW, bool BWD>
-__global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_walk_kernel(const ChunkArgs<T> a,
-                                                                    const GdrKeep keep)
+__device__ __forceinline__ void gdr_walk(const ChunkArgs<T>& a, const GdrKeep& keep, int block, char* lds)
 {
     using Sh = WalkLds<T, DK, NCW, BWD>;
     constexpr int P = Sh::P, KS = Sh::KSTEPS, KT = Sh::KT;
     constexpr int REC = gdr_rec_bytes<T, BWD>();
     constexpr int TILES = DV / (16 * NCW);  // workgroups of a chain
-    __shared__ __align__(16) char lds[Sh::NBUF * Sh::BYTES];
     // workgroups of one chain get indexes congruent modulo 8: one XCD, one L2 copy of K, Q and records
     const int chains = a.seq.N * a.H;
-    const int chain = blockIdx.x / (8 * TILES) * 8 + blockIdx.x % 8, tile = blockIdx.x / 8 % TILES;
+    const int chain = block / (8 * TILES) * 8 + block % 8, tile = block / 8 % TILES;
     if (chain >= chains) return;
     const int n = chain / a.H, h = chain % a.H, hk = h / a.rep;
     int t0, t1;
@@ -418,13 +416,27 @@ __global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_walk_kernel(const ChunkA
             for (int r = 0; r < 4; ++r) a.S_T[sbase + (size_t)(16 * k + r) * DV] = S[k][r] * sS.i;
 }
 
+template <class T, int DK, int DV, int NCW, int NLW, bool BWD>
+__global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_walk_kernel(const ChunkArgs<T> a,
+                                                                    const GdrKeep keep)
+{
+    using Sh = WalkLds<T, DK, NCW, BWD>;
+    __shared__ __align__(16) char lds[Sh::NBUF * Sh::BYTES];
+    gdr_walk<T, DK, DV, NCW, NLW, BWD>(a, keep, blockIdx.x, lds);
+}
+
+// Workgroups of a walk, in either direction.
+template <int DV, int NCW>
+unsigned walk_grid(const GdrSeq& s, int H)
+{
+    return (unsigned)((s.N * H + 7) / 8 * 8 * (DV / (16 * NCW)));
+}
+
 template <bool BWD, class T, int DK, int DV, int NCW, int NLW>
 hipError_t launch_gdr_walk(const ChunkArgs<T>& a, const GdrKeep& keep, hipStream_t stream)
 {
-    constexpr int TILES = DV / (16 * NCW);
-    const unsigned grid = (unsigned)((a.seq.N * a.H + 7) / 8 * 8 * TILES);
-    hipLaunchKernelGGL((gdr_walk_kernel<T, DK, DV, NCW, NLW, BWD>), dim3(grid), dim3(64 * (NCW + NLW)), 0,
-                       stream, a, keep);
+    hipLaunchKernelGGL((gdr_walk_kernel<T, DK, DV, NCW, NLW, BWD>), dim3(walk_grid<DV, NCW>(a.seq, a.H)),
+                       dim3(64 * (NCW + NLW)), 0, stream, a, keep);
     return hipGetLastError();
 }
 
