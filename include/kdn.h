@@ -329,7 +329,7 @@ kdn_status_t kdn_forward_kam(const void* q, const void* k, const void* v, const 
  *   workspace: kdn_forward_gdr_workspace_bytes(...) bytes (may be 0), 16-byte aligned, no
  *   initialisation needed.
  * Packing, alignment, asynchrony and errors as for kdn_forward_diag; there is no limit of 2 GiB on
- * a tensor, but H <= 65535 and N H <= 2^20 (KDN_ERR_UNSUPPORTED otherwise, as in the two calls
+ * a tensor, but H <= 65535 and N H <= 2^19 (KDN_ERR_UNSUPPORTED otherwise, as in the two calls
  * below). o must overlap no input and no state.
  */
 kdn_status_t kdn_forward_gdr(const void* q, const void* k, const void* v, const void* alpha,

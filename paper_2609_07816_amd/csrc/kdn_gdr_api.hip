@@ -8,7 +8,7 @@ namespace {
 using namespace kdn;
 
 // Offsets within a chunk of 64 tokens have 32 bits; a grid at most 2^32 threads.
-bool heads_fit(int32_t N, int32_t H) { return H <= 65535 && (int64_t)N * H <= (1 << 20); }
+bool heads_fit(int32_t N, int32_t H) { return H <= 65535 && (int64_t)N * H <= (1 << 19); }
 
 kdn_status_t check_heads(int32_t N, int32_t H, int32_t Hk, int32_t dk, int32_t dv, kdn_dtype_t dtype,
                          float scale)
@@ -22,7 +22,7 @@ kdn_status_t check_heads(int32_t N, int32_t H, int32_t Hk, int32_t dk, int32_t d
                     dv);
     if (!(scale > 0.f)) return fail(KDN_ERR_INVALID_ARG, "scale must be positive (%g)", scale);
     if (!heads_fit(N, H))
-        return fail(KDN_ERR_UNSUPPORTED, "%d sequences of H=%d: at most 65535 heads, and 2^20 in all", N,
+        return fail(KDN_ERR_UNSUPPORTED, "%d sequences of H=%d: at most 65535 heads, and 2^19 in all", N,
                     H);
     return KDN_OK;
 }

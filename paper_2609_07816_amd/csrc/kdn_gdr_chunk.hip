@@ -15,7 +15,7 @@ hipError_t launch_t(const GdrCall& c, hipStream_t stream)
                             gdr_max_chunks(s.cu_seqlens != nullptr, s.N, s.T, s.B * s.T), c.scale,
                             (char*)c.workspace};
     const hipError_t e = launch_gdr_prep(a, c.dk, false, stream);
-    return e != hipSuccess ? e : launch_gdr_walk_dk<false>(a, GdrKeep{}, c.dk, c.dv, stream);
+    return e != hipSuccess ? e : launch_gdr_walk_dk(a, c.dk, c.dv, stream);
 }
 
 }  // namespace

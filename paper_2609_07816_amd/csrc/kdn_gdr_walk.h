@@ -416,13 +416,12 @@ __device__ __forceinline__ void gdr_walk(const ChunkArgs<T>& a, const GdrKeep& k
             for (int r = 0; r < 4; ++r) a.S_T[sbase + (size_t)(16 * k + r) * DV] = S[k][r] * sS.i;
 }
 
-template <class T, int DK, int DV, int NCW, int NLW, bool BWD>
-__global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_walk_kernel(const ChunkArgs<T> a,
-                                                                    const GdrKeep keep)
+template <class T, int DK, int DV, int NCW, int NLW>
+__global__ __launch_bounds__(64 * (NCW + NLW)) void gdr_walk_kernel(const ChunkArgs<T> a)
 {
-    using Sh = WalkLds<T, DK, NCW, BWD>;
+    using Sh = WalkLds<T, DK, NCW, false>;
     __shared__ __align__(16) char lds[Sh::NBUF * Sh::BYTES];
-    gdr_walk<T, DK, DV, NCW, NLW, BWD>(a, keep, blockIdx.x, lds);
+    gdr_walk<T, DK, DV, NCW, NLW, false>(a, GdrKeep{}, blockIdx.x, lds);
 }
 
 // Workgroups of a walk, in either direction.
@@ -432,35 +431,34 @@ unsigned walk_grid(const GdrSeq& s, int H)
     return (unsigned)((s.N * H + 7) / 8 * 8 * (DV / (16 * NCW)));
 }
 
-template <bool BWD, class T, int DK, int DV, int NCW, int NLW>
-hipError_t launch_gdr_walk(const ChunkArgs<T>& a, const GdrKeep& keep, hipStream_t stream)
+template <class T, int DK, int DV, int NCW, int NLW>
+hipError_t launch_gdr_walk(const ChunkArgs<T>& a, hipStream_t stream)
 {
-    hipLaunchKernelGGL((gdr_walk_kernel<T, DK, DV, NCW, NLW, BWD>), dim3(walk_grid<DV, NCW>(a.seq, a.H)),
-                       dim3(64 * (NCW + NLW)), 0, stream, a, keep);
+    hipLaunchKernelGGL((gdr_walk_kernel<T, DK, DV, NCW, NLW>), dim3(walk_grid<DV, NCW>(a.seq, a.H)),
+                       dim3(64 * (NCW + NLW)), 0, stream, a);
     return hipGetLastError();
 }
 
-template <bool BWD, class T, int DK>
-hipError_t launch_gdr_walk_dv(const ChunkArgs<T>& a, const GdrKeep& keep, int dv, hipStream_t stream)
+template <class T, int DK>
+hipError_t launch_gdr_walk_dv(const ChunkArgs<T>& a, int dv, hipStream_t stream)
 {
     switch (dv) {
-    case 16: return launch_gdr_walk<BWD, T, DK, 16, 1, 2>(a, keep, stream);
-    case 32: return launch_gdr_walk<BWD, T, DK, 32, 2, 2>(a, keep, stream);
-    case 64: return launch_gdr_walk<BWD, T, DK, 64, 2, 2>(a, keep, stream);
-    case 128: return launch_gdr_walk<BWD, T, DK, 128, 2, 2>(a, keep, stream);
+    case 16: return launch_gdr_walk<T, DK, 16, 1, 2>(a, stream);
+    case 32: return launch_gdr_walk<T, DK, 32, 2, 2>(a, stream);
+    case 64: return launch_gdr_walk<T, DK, 64, 2, 2>(a, stream);
+    case 128: return launch_gdr_walk<T, DK, 128, 2, 2>(a, stream);
     }
     return hipErrorInvalidValue;
 }
 
-template <bool BWD, class T>
-hipError_t launch_gdr_walk_dk(const ChunkArgs<T>& a, const GdrKeep& keep, int dk, int dv,
-                              hipStream_t stream)
+template <class T>
+hipError_t launch_gdr_walk_dk(const ChunkArgs<T>& a, int dk, int dv, hipStream_t stream)
 {
     switch (dk) {
-    case 16: return launch_gdr_walk_dv<BWD, T, 16>(a, keep, dv, stream);
-    case 32: return launch_gdr_walk_dv<BWD, T, 32>(a, keep, dv, stream);
-    case 64: return launch_gdr_walk_dv<BWD, T, 64>(a, keep, dv, stream);
-    case 128: return launch_gdr_walk_dv<BWD, T, 128>(a, keep, dv, stream);
+    case 16: return launch_gdr_walk_dv<T, 16>(a, dv, stream);
+    case 32: return launch_gdr_walk_dv<T, 32>(a, dv, stream);
+    case 64: return launch_gdr_walk_dv<T, 64>(a, dv, stream);
+    case 128: return launch_gdr_walk_dv<T, 128>(a, dv, stream);
     }
     return hipErrorInvalidValue;
 }

@@ -285,7 +285,7 @@ def test_too_many_heads():
     for f in (kdn.forward_gdr, kdn.backward_gdr):
         with pytest.raises(kdn.KdnError):
             f(*z, g, g)
-    R = (1 << 20) // 16 + 1  # rows of 16 heads
+    R = (1 << 19) // 16 + 1  # rows of 16 heads
     z = [torch.zeros(R, 1, 16, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
     v = torch.zeros(R, 16, 16, dtype=torch.bfloat16, device="cuda")
     g = torch.zeros(R, 16, dtype=torch.bfloat16, device="cuda")
