@@ -17,6 +17,9 @@ namespace {
 // 16 x 16 blocks by substitution (lane = column: T_bb = (I + M_bb beta)^-1 in one row of 16 lanes,
 // W_bb = T_bb M_bb in another), the others by block products
 // W_bc = T_bb (M_bc - sum_m M_bm beta_m W_mc), wave = block column.
+// Bound by its own latencies, one after another (loads, the decays' sums, products, the solve): 10 us for
+// two chunks, 36 us for 128 chunks of 16 heads of d 128, 75 us for 256 of them with the backward's records
+// (250 MB, 50 us at the copy rate).
 // ------------------------------------------------------------------------------------------
 constexpr int LP = 20;  // floats of a tile's row in LDS
 constexpr int MP = 68;  // floats of a matrix row in LDS

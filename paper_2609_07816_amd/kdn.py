@@ -118,11 +118,10 @@ def lib():
     L.kdn_beam_select_workspace_bytes.argtypes = [i32] * 3
     L.kdn_beam_select_workspace_bytes.restype = sz
     L.kdn_beam_reorder.argtypes = [vp] * 3 + [i32] * 3 + [vp, sz, vp, sz, vp]
-    for name in ("kdn_forward_gdr", "kdn_backward_gdr", "kdn_decode_step_gdr", "kdn_beam_select", "kdn_beam_reorder"):
-        getattr(L, name).restype = ctypes.c_int
     for name in ("kdn_forward_diag", "kdn_forward_iso", "kdn_forward_diag_noalloc",
                  "kdn_decode_step", "kdn_gain_diag", "kdn_gain_iso", "kdn_forward_layer",
-                 "kdn_decode_step_layer", "kdn_backward"):
+                 "kdn_decode_step_layer", "kdn_backward", "kdn_forward_gdr", "kdn_backward_gdr",
+                 "kdn_decode_step_gdr", "kdn_beam_select", "kdn_beam_reorder"):
         getattr(L, name).restype = ctypes.c_int
     L.kdn_forward_workspace_bytes.restype = sz
     L.kdn_gain_workspace_bytes.restype = sz
