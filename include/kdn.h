@@ -330,7 +330,9 @@ kdn_status_t kdn_forward_kam(const void* q, const void* k, const void* v, const 
  *   initialisation needed.
  * Packing, alignment, asynchrony and errors as for kdn_forward_diag; there is no limit of 2 GiB on
  * a tensor, but H <= 65535 and N H <= 2^19 (KDN_ERR_UNSUPPORTED otherwise, as in the two calls
- * below). o must overlap no input and no state.
+ * below), and B T H <= 2^24. o must overlap no input and no state.
+ * A value that is not finite may reach the other tokens of its 64 and everything after them (in the
+ * backward also before them), never another sequence.
  */
 kdn_status_t kdn_forward_gdr(const void* q, const void* k, const void* v, const void* alpha,
                              const void* beta, const float* S0, void* o, float* S_T,
