@@ -8,7 +8,7 @@
 // rows of 32 value columns (16 at dv = 16) and no two wavefronts exchange anything: a lane has dk / 8
 // rows of four adjacent columns, so a load of the state is 16 bytes per lane and whole 128-byte row
 // pieces. A decode step is bound by HBM, which S crosses once in and once out: 256 rows of 16 heads of
-// d 128 in 117 us, 4.6 TB/s, 93% of a large copy's rate; 4 rows in 9 us, a launch and one round trip.
+// d 128 in 117 us, 4.6 TB/s, 96% of a large copy's rate; 4 rows in 9 us, a launch and one round trip.
 #include "kdn_gdr.h"
 
 namespace kdn {
