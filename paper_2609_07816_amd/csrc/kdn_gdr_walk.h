@@ -12,10 +12,9 @@
 // Bound by the chain: a wavefront's own sequence of some 600 vector and 104 matrix instructions per chunk
 // (d 128) and the LDS reads between them, 2.5 us a chunk, which no other wavefront can take over: 64 chunks
 // of 4 sequences of 16 heads 165 us at full clocks (205 soon after a start), 128 chunks of one 340 us, of 40
-// and 10 us of bytes. 32 columns a
-// workgroup fill the card with 64 chains (4 x 16 heads); 16 columns measured 357 against 372 us for the
-// one sequence and 388 against 234 us for the four (whole calls). Loaders of 3 and 4 waves, direct loads
-// into LDS, and waves of their own for the output were slower.
+// and 10 us of bytes. 32 columns a workgroup fill the card with 64 chains (4 x 16 heads); 16 columns
+// measured 357 against 372 us for the one sequence and 388 against 234 us for the four (whole calls).
+// Loaders of 3 and 4 waves, direct loads into LDS, and waves of their own for the output were slower.
 #pragma once
 
 #include "kdn_gdr_device.h"
